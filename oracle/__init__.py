@@ -40,6 +40,8 @@ Contents (all float64 unless stated):
                      the token recurrence, the chunk form of eq. chunk-state,
                      and trajectory-wise execution over a forest with
                      gradients by reverse mode.
+* ``gen``         -- generation over a forest of cached segments: e4m3 rounding,
+                     attention of the last rows of segments, recurrent steps.
 
 Recurrence reading used by every module but ``kda`` (the paper prints only
 KDA's chunk update, eq. chunk-state): S_t = exp(g_t) S_{t-1} + k_t v_t^T and o_t = scale S_t^T q_t,

@@ -5,4 +5,4 @@ kernels for gfx950.  This package is its thin Python binding.
 """
 from . import _lib  # noqa: F401
 
-__all__ = ["plan", "tree_la"]
+__all__ = ["plan", "rollout", "tree_la"]

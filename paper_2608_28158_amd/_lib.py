@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("HARTS_LIB", os.path.join(HERE, "libharts.so"))
 
 HARTS_OK, HARTS_EINVAL, HARTS_EUNSUPPORTED, HARTS_EHIP, HARTS_ENOMEM = 0, -1, -2, -3, -4
-HARTS_F32, HARTS_BF16 = 0, 1
+HARTS_F32, HARTS_BF16, HARTS_E4M3 = 0, 1, 2
 
 # Every symbol include/harts.h declares.
 EXPORTS = (
@@ -29,6 +29,8 @@ EXPORTS = (
     "harts_attn_bwd", "harts_attn_scatter",
     "harts_kda_layout", "harts_kda_tables", "harts_kda_workspace_size", "harts_kda_fwd", "harts_kda_bwd",
     "harts_kda_bank_add", "harts_kda_reduce",
+    "harts_cache_write", "harts_cache_read", "harts_gen_layout", "harts_gen_tables",
+    "harts_gen_workspace_size", "harts_gen_attn", "harts_la_step", "harts_kda_step",
     "harts_profile_begin", "harts_profile_end",
 )
 
@@ -100,6 +102,15 @@ class AttnLayout(C.Structure):
 class KdaSizes(C.Structure):
     _fields_ = [("n_chunks", C.c_int64), ("n_slots", C.c_int64)] + \
         [(n, C.c_int32) for n in ("n_seq", "n_rounds", "n_groups", "n_req", "n_multi", "pad")]
+
+
+class Cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_exp", "v_exp", "pages", "len")] + \
+        [(n, C.c_int32) for n in ("n_pages", "n_seg", "pitch", "H", "d", "kind")]
+
+
+class GenSizes(C.Structure):
+    _fields_ = [(n, C.c_int64) for n in ("n_rows", "n_items", "n_parts", "n_join")]
 
 
 class KernelTime(C.Structure):
@@ -206,6 +217,22 @@ def lib():
     L.harts_kda_bank_add.argtypes = [vp, i32, i32, vp, i64, vp, vp, vp]
     L.harts_kda_reduce.restype = C.c_int
     L.harts_kda_reduce.argtypes = [vp, vp, vp, i64, i64, i32, vp, vp]
+    L.harts_cache_write.restype = C.c_int
+    L.harts_cache_write.argtypes = [vp, vp, i64, vp, vp, vp]
+    L.harts_cache_read.restype = C.c_int
+    L.harts_cache_read.argtypes = [vp, vp, i64, vp, vp, vp]
+    L.harts_gen_layout.restype = C.c_int
+    L.harts_gen_layout.argtypes = [i32, vp, vp, vp, i32, i32, vp]
+    L.harts_gen_tables.restype = C.c_int
+    L.harts_gen_tables.argtypes = [i32, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+    L.harts_gen_workspace_size.restype = C.c_int
+    L.harts_gen_workspace_size.argtypes = [vp, i32, i32, C.POINTER(sz)]
+    L.harts_gen_attn.restype = C.c_int
+    L.harts_gen_attn.argtypes = [vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, vp, sz, vp]
+    L.harts_la_step.restype = C.c_int
+    L.harts_la_step.argtypes = [i32, i64, i64, i32, i32, f32] + [vp] * 7 + [i64, vp, vp, i64, vp, vp]
+    L.harts_kda_step.restype = C.c_int
+    L.harts_kda_step.argtypes = [i32, i64, i64, i32, i32, f32] + [vp] * 8 + [i64, vp, vp, i64, vp, vp]
     L.harts_profile_begin.restype = C.c_int
     L.harts_profile_begin.argtypes = []
     L.harts_profile_end.restype = C.c_int
