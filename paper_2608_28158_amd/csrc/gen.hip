@@ -7,40 +7,49 @@
 //                its largest magnitude with shuffles;
 //   k_gen_attn   a workgroup of 4 waves per (work item, key head): a tile of
 //                stacked rows (query rows x query heads of the key head)
-//                against one split of a segment's keys;
+//                against one split of a segment's keys, in one of two ways;
 //   k_gen_join   joins the parts of rows that have several.
 //
-// k_gen_attn keeps everything but the final join in registers.  Products are
-// issued with the roles that leave a stacked row in a lane's column: S^T = K Q^T
-// and O^T = V^T P^T, bf16 MFMA 16x16x32.  Then
-//   - a row's maximum, sum, weights and outputs stay in the lanes of one column
-//     (lane % 16 = row; the four lane groups g hold different keys);
-//   - two 16-key score tiles are the B operand of the second product as they
-//     stand, with slot (g, e) of its 32-deep contraction meaning key 4g + e
-//     (e < 4) or 16 + 4g + e - 4, so the weights never leave their lane;
-//   - V^T fragments need 8 such keys of one column per lane.  A lane reads the
-//     8 rows' D / 16 neighbouring columns (whole rows across the 16 lanes of a
-//     group) and transposes them with byte permutes: fragment j holds column
+// Products are issued with the roles that leave a stacked row in a lane's
+// column: S^T = K Q^T and O^T = V^T P^T, bf16 MFMA 16x16x32.  A row's maximum,
+// sum, weights and outputs then stay in the lanes of one column (lane % 16 =
+// row; the four lane groups g hold different keys), and two 16-key score tiles
+// are the B operand of the second product as they stand, with slot (g, e) of
+// its 32-deep contraction meaning key 4g + e (e < 4) or 16 + 4g + e - 4.
+//
+// Few rows (gen_few): the item is bound by reading the keys and values, so
+// nothing stands between memory and the products.  A wave has 16 rows and every
+// second or fourth 32-key step, straight from the cache into registers, with no
+// LDS and no barrier in the loop; the next step is requested as soon as this
+// one's registers are free, and the waves join through LDS at the end.
+//   - V^T fragments need 8 keys of one column per lane.  A lane reads 8 rows'
+//     D / 16 neighbouring columns (whole rows across the 16 lanes of a group)
+//     and transposes them with byte permutes: fragment j holds column
 //     (lane % 16) D / 16 + j, and a lane's outputs are D / 4 neighbouring
 //     columns of its row;
 //   - K fragments are 16-byte reads along d; the contraction order of the first
 //     product is free, so the 8-bit cache is read 16 bytes a lane too and Q is
 //     read in the matching order.
-// No LDS and no barrier in the loop: the keys of the next 32-key step are
-// requested as soon as this step's registers are free.  The exponent reference
-// of a row moves only when a score exceeds it by 2^8, as the largest weight
-// that leaves sums and products far from overflow; most steps then have no
-// rescale and no exchange between lanes.  Weights are rounded to bf16 for the
-// second product (relative 2^-9 each, as every product of bf16 operands), their
-// sum is taken before that in float32.
+// Many rows (gen_many): a wave has 32 rows, the four waves share each step's
+// keys through LDS, double-buffered with one barrier a step: bf16 rows are
+// loaded straight into it, 8-bit ones on their way through registers, where
+// they become bf16 once for all waves.
+//
+// The exponent reference of a row moves only when a score exceeds it by 2^8, as
+// the largest weight that leaves sums and products far from overflow; most
+// steps then have no rescale and no exchange between lanes.  Weights are
+// rounded to bf16 for the second product (half a step, 2^-8 of each, as any
+// bf16 operand); their sum is taken before that in float32.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "gen.hpp"
 #include "harts.h"
 #include "la_common.hpp"
+#include "lds_load.hpp"
 #include "plan.hpp"
 
 namespace harts {
@@ -313,6 +322,16 @@ __device__ inline u32 pack_bf16(float a, float b) {
   return __builtin_bit_cast(u32, x);
 }
 
+// natural logarithm of sum * 2^ref
+__device__ inline float log_sum(float ref, float sum) {
+  return sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * GEN_LN2;
+}
+
+// Tables that the whole wave reads at one address, through the scalar cache: the
+// read then waits for none of the requests for keys that are out.
+typedef const __attribute__((address_space(4))) int32_t* Scalars;
+__device__ inline Scalars scalars(const int32_t* p) { return (Scalars)p; }
+
 struct GenArgs {
   CacheView c;
   const int32_t *items, *order, *part_off;
@@ -323,77 +342,140 @@ struct GenArgs {
   float *lse, *acc, *ml;       // acc [parts][Hq][D], ml [parts][Hq][2]
 };
 
-// Floats of one wave's results in LDS: maximum, sum and accumulators of T tiles.
-template <int D, int T> constexpr int join_floats() { return (2 * T + T * D / 4) * 64; }
+// What an item's rows see: rows of the segment that exist (n), all that were
+// written or are to come (cached), its own new rows.
+struct Reach {
+  int64_t cached;
+  int32_t n, n_new;
+  __device__ inline Reach(const CacheView& c, int32_t seg, int32_t n_new_) : n_new(n_new_) {
+    cached = max(scalars(c.len)[seg], 0);
+    n = static_cast<int32_t>(min(min(cached, static_cast<int64_t>(c.pitch) * GEN_PAGE),
+                                 static_cast<int64_t>(INT32_MAX - GEN_PAGE)));
+  }
+  // keys that the row at a place below the segment sees
+  __device__ inline int32_t of(int32_t place) const {
+    const int64_t own = cached - n_new + place + 1;
+    return place < n_new ? static_cast<int32_t>(max(int64_t{0}, min(own, static_cast<int64_t>(n)))) : n;
+  }
+};
 
-// One work item by waves of T row tiles.  kw: the wave's turn among the KW that
-// share the keys of its rows; rt: its place along the rows.
-template <int D, bool E4M3, int T>
-__device__ inline void gen_item(const GenArgs& A, const int32_t* __restrict__ it, int hk, int wave, int lane,
-                                float* __restrict__ lds) {
+// The item's steps [from, to) of T keys, of those up to key `hi`.
+template <int T>
+__device__ inline void split_steps(Scalars it, int32_t hi, int32_t& from, int32_t& to) {
+  const int32_t steps = (hi + T - 1) / T, n = it[GI_SPLITS];
+  const int32_t per = (steps + n - 1) / n;
+  from = static_cast<int32_t>(min(static_cast<int64_t>(it[GI_SPLIT]) * per, static_cast<int64_t>(steps)));
+  to = min(from + per, steps);
+}
+
+// Key of element e of a fragment of 32 keys, for lane group g.
+__device__ inline int frag_key(int g, int e) { return 4 * g + (e < 4 ? e : 12 + e); }
+
+// A pair of bf16 without its values that are not finite (exponent all ones);
+// `odd` gets a bit if it had one.
+__device__ inline u32 finite_pair(u32 w, u32& odd) {
+  const u32 t = ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  odd |= t;
+  return w & ~((t - (t >> 15)) | t);
+}
+
+__device__ inline float over_groups_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ inline float over_groups_sum(float x) {
+  x += __shfl_xor(x, 16);
+  return x + __shfl_xor(x, 32);
+}
+
+// A row's running reference and sum, with the accumulators of DT tiles.
+template <int DT>
+struct RowState {
+  float ref, sum;
+  f32x4 acc[DT];
+  __device__ inline void clear() {
+    ref = -INFINITY;
+    sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < DT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  // the reference rises to the rows' maxima
+  __device__ inline void raise(float top) {
+    const float to = fmaxf(ref, over_groups_max(top));
+    const float f = to == ref ? 1.f : __builtin_amdgcn_exp2f(ref - to);
+    ref = to;
+    sum *= f;
+#pragma unroll
+    for (int j = 0; j < DT; ++j) acc[j] *= f;
+  }
+  __device__ inline float zero_point() const { return ref == -INFINITY ? 0.f : ref; }
+};
+
+// Values that are not finite, in steps whose keys some rows of a wave see and
+// others do not (a weight of 0 times infinity would not be 0): the products of
+// such steps leave them out, and afterwards they are added, as they are, to the
+// columns [c0, c0 + cols) of the output row (o, or a part's accumulators) that
+// the lane has written, if the row sees them.
+template <int D, bool E4M3, typename T>
+__device__ inline void add_odd(const CacheView& c, Scalars table, int hk, int32_t key0, int32_t keys, int32_t n,
+                               int32_t lim, T* out, int c0, int cols) {
+  const int32_t page = table[key0 / GEN_PAGE];
+  if (page < 0 || page >= c.n_pages) return;
+  const int64_t row0 = (static_cast<int64_t>(page) * c.H + hk) * GEN_PAGE + key0 % GEN_PAGE;
+#pragma unroll 1
+  for (int32_t k = 0; k < keys && key0 + k < min(n, lim); ++k)
+#pragma unroll 1
+    for (int j = c0; j < c0 + cols; ++j) {
+      const int64_t at = (row0 + k) * D + j;
+      float x;
+      if constexpr (E4M3) x = (reinterpret_cast<const uint8_t*>(c.v)[at] & 0x7fu) == 0x7fu ? __builtin_nanf("") : 0.f;
+      else x = static_cast<float>(reinterpret_cast<const bf16*>(c.v)[at]);
+      if (!(fabsf(x) < INFINITY)) out[j] = static_cast<T>(static_cast<float>(out[j]) + x);
+    }
+}
+
+constexpr int GEN_JOIN = 35;   // floats a lane leaves in LDS for a join at D = 128
+
+// Few rows: 16 of them a wave; GI_WAVES waves along the rows, the others share
+// the keys.
+template <int D, bool E4M3>
+__device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, int lane,
+                               float* __restrict__ lds) {
   typedef KvStep<D, E4M3> Step;
   constexpr int DT = D / 16;                        // 16-column tiles
+  static_assert(3 + 4 * DT <= GEN_JOIN, "room for a join");
   const CacheView& c = A.c;
   const int rw = it[GI_WAVES], kws = 4 / rw;
   const int rt = wave % rw, kw = wave / rw;
-  const int seg = it[GI_SEG], n_new = it[GI_NEW], group = A.Hq / c.H;
+  const int seg = it[GI_SEG], group = A.Hq / c.H;
   const int g = lane >> 4, i = lane & 15;
+  const Reach reach(c, seg, it[GI_NEW]);
+  const int32_t n = reach.n;
 
-  // rows of this lane's columns
-  const int64_t cached = c.len[seg] < 0 ? 0 : c.len[seg];
-  const int64_t held = min(cached, static_cast<int64_t>(c.pitch) * GEN_PAGE);
-  const int32_t n = static_cast<int32_t>(min(held, static_cast<int64_t>(INT32_MAX - 64)));
-  int32_t row[T], head[T], lim[T];
-  bool live[T];
-  bf16x8 qf[T][D / 32];
-  int32_t lo = n, hi = 0;
+  const int local = 16 * rt + i;
+  const bool live = local < it[GI_N];
+  const int stacked = it[GI_ROW] + (live ? local : 0), place = stacked / group;
+  const int32_t row = A.order[it[GI_FIRST] + place], head = hk * group + stacked % group;
+  int32_t lim = reach.of(place);
+  bf16x8 qf[D / 32];
+  const bf16* qp = A.q + (static_cast<int64_t>(row) * A.Hq + head) * D;
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    const int local = 16 * (rt * T + t) + i;
-    live[t] = local < it[GI_N];
-    const int stacked = it[GI_ROW] + (live[t] ? local : 0);
-    const int place = stacked / group;              // among the rows below the segment
-    row[t] = A.order[it[GI_FIRST] + place];
-    head[t] = hk * group + stacked % group;
-    const int64_t own = cached - n_new + place + 1; // rows up to its own
-    lim[t] = place < n_new ? static_cast<int32_t>(max(int64_t{0}, min(own, static_cast<int64_t>(n)))) : n;
-    if (!live[t]) lim[t] = -1;
-    hi = max(hi, lim[t]);
-    if (live[t]) lo = min(lo, lim[t]);
-    const bf16* qp = A.q + (static_cast<int64_t>(row[t]) * A.Hq + head[t]) * D;
-#pragma unroll
-    for (int s = 0; s < D / 32; ++s) qf[t][s] = *reinterpret_cast<const bf16x8*>(qp + Step::k_col(s, g));
-  }
-#pragma unroll
-  for (int s = 1; s < 16; s *= 2) {
-    hi = max(hi, __shfl_xor(hi, s));
-    lo = min(lo, __shfl_xor(lo, s));
-  }
-  hi = __builtin_amdgcn_readfirstlane(hi);
-  lo = __builtin_amdgcn_readfirstlane(lo);
-#pragma unroll
-  for (int t = 0; t < T; ++t)
-    if (!live[t]) lim[t] = INT32_MAX;               // padding rows take part unmasked and are dropped
+  for (int s = 0; s < D / 32; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + Step::k_col(s, g));
+  // the fewest and the most keys that a row of the wave sees: places grow along
+  // it, and what a row sees with its place (own rows one more each, then the
+  // descendants', which see all)
+  const int first = 16 * rt, last = min(first + 16, it[GI_N]) - 1;
+  const int32_t lo = last < first ? n : reach.of((it[GI_ROW] + first) / group);
+  const int32_t hi = last < first ? 0 : reach.of((it[GI_ROW] + last) / group);
+  if (!live) lim = n;                               // padding rows take part and are dropped
 
-  // this wave's steps: the item's share of the steps that some row of the
-  // workgroup's tile can see would differ between waves; hi of the wave is
-  // enough, as rows of a wave see no key past it
-  const int32_t steps = (hi + 31) / 32;
-  const int32_t per = (((n + 31) / 32) + it[GI_SPLITS] - 1) / it[GI_SPLITS];
-  const int64_t from = static_cast<int64_t>(it[GI_SPLIT]) * per;
-  const int32_t end = static_cast<int32_t>(min(from + per, static_cast<int64_t>(steps)));
+  int32_t from, end;
+  split_steps<32>(it, hi, from, end);
+  RowState<DT> st;
+  st.clear();
+  bool odds = false;
 
-  f32x4 acc[T][DT];
-  float ref[T], sum[T];
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    ref[t] = -INFINITY;
-    sum[t] = 0.f;
-#pragma unroll
-    for (int j = 0; j < DT; ++j) acc[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  const int32_t* table = c.pages + static_cast<int64_t>(seg) * c.pitch;
+  const Scalars table = scalars(c.pages) + static_cast<int64_t>(seg) * c.pitch;
   const auto page_of = [&](int32_t u) {
     const int32_t p = table[u >> 1];
     return p >= 0 && p < c.n_pages ? p : -1;
@@ -402,207 +484,409 @@ __device__ inline void gen_item(const GenArgs& A, const int32_t* __restrict__ it
     return (static_cast<int64_t>(page < 0 ? 0 : page) * c.H + hk) * GEN_PAGE;
   };
   Step x;
-  int64_t u = from + kw;
-  int32_t page = -1;
+  int32_t u = from + kw, page = -1;
   if (u < end) {
-    page = page_of(static_cast<int32_t>(u));
+    page = page_of(u);
     const int64_t b = base_of(page);
     x.load_k(c.k + b * Step::ROWB, c.ke + b, u & 1, lane);
     x.load_v(c.v + b * Step::ROWB, c.ve + b, u & 1, lane);
   }
   for (; u < end; u += kws) {
-    const int32_t key0 = static_cast<int32_t>(u) * 32;
+    const int32_t key0 = u * 32;
     const bool more = u + kws < end;
-    const int32_t next = more ? page_of(static_cast<int32_t>(u + kws)) : page;
+    const int32_t next = more ? page_of(u + kws) : page;
     const int64_t nb = base_of(next);
-    const int nhalf = more ? static_cast<int>((u + kws) & 1) : static_cast<int>(u & 1);
+    const int nhalf = (more ? u + kws : u) & 1;
 
-    f32x4 s[T][2];
-#pragma unroll
-    for (int t = 0; t < T; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) {
-        const bf16x8 kf = x.k_frag(kt, d);
-#pragma unroll
-        for (int t = 0; t < T; ++t) s[t][kt] = mfma32(kf, qf[t][d], s[t][kt]);
-      }
+      for (int d = 0; d < D / 32; ++d) s[kt] = mfma32(x.k_frag(kt, d), qf[d], s[kt]);
     x.load_k(c.k + nb * Step::ROWB, c.ke + nb, nhalf, lane);
 
     const bool edge = key0 + 32 > lo || page < 0;   // some key is hidden from some row
-    u32x4 w[T];
+    float y[8], top = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      float y[8], top = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[e] = s[t][e >> 2][e & 3] * A.scale;
-        if (edge) {
-          const int32_t key = key0 + 4 * g + (e < 4 ? e : 12 + e);
-          if (key >= lim[t] || key >= n || page < 0) y[e] = -INFINITY;
-        }
-        top = fmaxf(top, y[e]);
-      }
-      if (__any(top > ref[t] + GEN_SLACK)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float to = fmaxf(ref[t], top);
-        const float f = to == -INFINITY || to == ref[t] ? 1.f : __builtin_amdgcn_exp2f(ref[t] - to);
-        ref[t] = to;
-        sum[t] *= f;
-#pragma unroll
-        for (int j = 0; j < DT; ++j) acc[t][j] *= f;
-      }
-      const float r = ref[t] == -INFINITY ? 0.f : ref[t];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        y[e] = __builtin_amdgcn_exp2f(y[e] - r);
-        sum[t] += y[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[t][e] = pack_bf16(y[2 * e], y[2 * e + 1]);
+    for (int e = 0; e < 8; ++e) {
+      y[e] = s[e >> 2][e & 3] * A.scale;
+      if (edge && (key0 + frag_key(g, e) >= lim || page < 0)) y[e] = -INFINITY;
+      top = fmaxf(top, y[e]);
     }
+    if (__any(top > st.ref + GEN_SLACK)) st.raise(top);
+    const float r = st.zero_point();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] = __builtin_amdgcn_exp2f(y[e] - r);
+      st.sum += y[e];
+    }
+    const bf16x8 w = __builtin_bit_cast(
+        bf16x8, u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])});
 
     u32 vw[8][Step::VW];
     x.v_rows(vw);
-    bool apart = false;
     if (edge) {
-      // rows that do not exist hold anything: zeros, since a weight of 0 times
-      // infinity would not be 0
-      bool odd = false;
+      // (rows that do not exist hold anything)
+      u32 odd = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool there = page >= 0 && key0 + 4 * g + (e < 4 ? e : 12 + e) < n;
+        const bool there = page >= 0 && key0 + frag_key(g, e) < n;
 #pragma unroll
-        for (int q = 0; q < Step::VW; ++q) {
-          vw[e][q] = there ? vw[e][q] : 0u;
-          odd |= (vw[e][q] & 0x7f80u) == 0x7f80u || (vw[e][q] & 0x7f800000u) == 0x7f800000u;
-        }
+        for (int q = 0; q < Step::VW; ++q) vw[e][q] = there ? finite_pair(vw[e][q], odd) : 0u;
       }
-      // new rows that are not finite, in a step whose keys some of the rows see
-      // and others do not
-      apart = lo < min(hi, key0 + 32) && __any(odd);
+      odds |= __any(odd != 0);
     }
-    if (!apart) {
 #pragma unroll
-      for (int j = 0; j < DT; ++j) {
-        const bf16x8 vf = v_frag(vw, j);
-#pragma unroll
-        for (int t = 0; t < T; ++t) acc[t][j] = mfma32(vf, __builtin_bit_cast(bf16x8, w[t]), acc[t][j]);
-      }
-    } else {
-      // one column (row) at a time, with the keys that it does not see as zeros
-#pragma unroll
-      for (int t = 0; t < T; ++t)
-#pragma unroll 1
-        for (int col = 0; col < 16; ++col) {
-          const int32_t most = __shfl(lim[t], col);
-#pragma unroll
-          for (int q = 0; q < Step::VW; ++q) {
-            u32 vz[8][1];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) vz[e][0] = key0 + 4 * g + (e < 4 ? e : 12 + e) < most ? vw[e][q] : 0u;
-#pragma unroll
-            for (int j = 2 * q; j < 2 * q + 2; ++j) {
-              const f32x4 y = mfma32(v_frag(vz, j & 1), __builtin_bit_cast(bf16x8, w[t]), acc[t][j]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[t][j][e] = i == col ? y[e] : acc[t][j][e];
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-    }
+    for (int j = 0; j < DT; ++j) st.acc[j] = mfma32(v_frag(vw, j), w, st.acc[j]);
     x.load_v(c.v + nb * Step::ROWB, c.ve + nb, nhalf, lane);
     page = next;
   }
-
-#pragma unroll
-  for (int t = 0; t < T; ++t) {
-    sum[t] += __shfl_xor(sum[t], 16);
-    sum[t] += __shfl_xor(sum[t], 32);
-  }
+  st.sum = over_groups_sum(st.sum);
 
   // join the waves that shared the keys, half of them into the other half
   for (int step = kws / 2; step >= 1; step /= 2) {
-    constexpr int F = join_floats<D, T>();
     if (kw >= step && kw < 2 * step) {
-      float* p = lds + static_cast<int64_t>((kw - step) * rw + rt) * F + lane;
+      float* p = lds + ((kw - step) * rw + rt) * (64 * GEN_JOIN) + lane;
+      p[0] = st.ref;
+      p[64] = st.sum;
+      p[128] = odds ? 1.f : 0.f;
 #pragma unroll
-      for (int t = 0; t < T; ++t) {
-        p[64 * (2 * t)] = ref[t];
-        p[64 * (2 * t + 1)] = sum[t];
+      for (int j = 0; j < DT; ++j)
 #pragma unroll
-        for (int j = 0; j < DT; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[64 * (2 * T + (t * DT + j) * 4 + e)] = acc[t][j][e];
-      }
+        for (int e = 0; e < 4; ++e) p[64 * (3 + 4 * j + e)] = st.acc[j][e];
     }
     __syncthreads();
     if (kw < step) {
-      const float* p = lds + static_cast<int64_t>(kw * rw + rt) * F + lane;
+      const float* p = lds + (kw * rw + rt) * (64 * GEN_JOIN) + lane;
+      const float r1 = p[0], s1 = p[64], to = fmaxf(st.ref, r1), r = to == -INFINITY ? 0.f : to;
+      const float f0 = __builtin_amdgcn_exp2f(st.ref - r), f1 = __builtin_amdgcn_exp2f(r1 - r);
+      st.ref = to;
+      st.sum = st.sum * f0 + s1 * f1;
+      odds |= p[128] != 0.f;
 #pragma unroll
-      for (int t = 0; t < T; ++t) {
-        const float r1 = p[64 * (2 * t)], s1 = p[64 * (2 * t + 1)];
-        const float to = fmaxf(ref[t], r1);
-        const float r = to == -INFINITY ? 0.f : to;
-        const float f0 = __builtin_amdgcn_exp2f(ref[t] - r), f1 = __builtin_amdgcn_exp2f(r1 - r);
-        ref[t] = to;
-        sum[t] = sum[t] * f0 + s1 * f1;
+      for (int j = 0; j < DT; ++j)
 #pragma unroll
-        for (int j = 0; j < DT; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[t][j][e] = acc[t][j][e] * f0 + p[64 * (2 * T + (t * DT + j) * 4 + e)] * f1;
-      }
+        for (int e = 0; e < 4; ++e) st.acc[j][e] = st.acc[j][e] * f0 + p[64 * (3 + 4 * j + e)] * f1;
     }
     if (step > 1) __syncthreads();
   }
-  if (kw != 0) return;
+  if (kw != 0 || !live) return;
+
+  const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
+  if (parts == 1) {
+    const int64_t rh = static_cast<int64_t>(row) * A.Hq + head;
+    const float f = st.sum == 0.f ? 0.f : 1.f / st.sum;
+    u32 out[D / 8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int j = 0; j < DT; j += 2)
+        out[e * (DT / 2) + j / 2] = pack_bf16(st.acc[j][e] * f, st.acc[j + 1][e] * f);
+    u32x4* op = reinterpret_cast<u32x4*>(A.o + rh * D + g * (D / 4));
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) op[e] = u32x4{out[4 * e], out[4 * e + 1], out[4 * e + 2], out[4 * e + 3]};
+    if (A.lse && g == 0) A.lse[rh] = log_sum(st.ref, st.sum);
+    if (odds)
+      for (u = max(from, lo / 32); u < end; ++u)
+        add_odd<D, E4M3>(c, table, hk, u * 32, 32, n, lim, A.o + rh * D, g * (D / 4), D / 4);
+  } else {
+    const int64_t at = (static_cast<int64_t>(p0) + it[GI_PART] + it[GI_SPLIT]) * A.Hq + head;
+    f32x4* ap = reinterpret_cast<f32x4*>(A.acc + at * D + g * (D / 4));
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int j = 0; j < DT; j += 4)
+        ap[(e * DT + j) / 4] = f32x4{st.acc[j][e], st.acc[j + 1][e], st.acc[j + 2][e], st.acc[j + 3][e]};
+    if (g == 0) {
+      A.ml[2 * at] = st.ref;
+      A.ml[2 * at + 1] = st.sum;
+    }
+    if (odds)
+      for (u = max(from, lo / 32); u < end; ++u)
+        add_odd<D, E4M3>(c, table, hk, u * 32, 32, n, lim, A.acc + at * D, g * (D / 4), D / 4);
+  }
+}
+
+// LDS tile of T keys x D bf16, unpadded.  Row r keeps its 16-byte piece p at
+// slot p ^ swz(r), chosen for the lanes that the LDS serves together: a 16-byte
+// fragment read takes sets of rows r and r ^ 12 at neighbouring pieces, a
+// transposed read 8 rows of two neighbouring pieces (both free of conflicts).
+template <int D>
+struct GenTile {
+  static constexpr int PPR = D / 8;
+  __device__ static inline int swz(int r) {
+    const int hi = (r >> 3) & 1;
+    return D == 128 ? (((r & 7) ^ (hi << 2)) << 1) | hi : ((r & 6) ^ (hi << 2)) | hi;
+  }
+  // lane (g, i): key k0 + i (k0 a multiple of 16), columns 32 s + 8 g .. + 7
+  __device__ static inline bf16x8 rows(const bf16* t, int k0, int s, int lane) {
+    typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+    const int i = lane & 15, g = lane >> 4;
+    return *(const lds_bf16x8*)(t + (k0 + i) * D + (((4 * s + g) ^ swz(i)) << 3));
+  }
+  // lane (g, i): column c0 + i, keys k0 + frag_key(g, 0 .. 7)
+  __device__ static inline bf16x8 columns(const bf16* t, int k0, int c0, int lane) {
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const int r = (lane >> 4) * 4 + ((lane & 15) >> 2), c = lane & 3;
+    const bf16* p = t + (k0 + r) * D + ((((c0 >> 3) + (c >> 1)) ^ swz(r)) << 3) + 4 * (c & 1);
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * D));
+    return Frag<bf16>::join(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi));
+  }
+};
+
+// Requests of T cached rows of one page half (or page) into a tile.  Thread t
+// fills the 16-byte slots t, t + 256, ...: of rows r0, r0 + RPE, ...
+template <int D, int T, bool E4M3> struct GenStage;
+
+template <int D, int T> struct GenStage<D, T, false> {
+  static constexpr int RPE = GEN_THR / (D / 8), N = T / RPE;
+  static_assert(RPE % 16 == 0, "every request starts at a multiple of 16 rows");
+  int r0, wave;
+  u32 off;
+  __device__ inline GenStage(int t, int wave_) : r0(t / (D / 8)), wave(wave_) {
+    off = r0 * (2 * D) + 16 * ((t % (D / 8)) ^ GenTile<D>::swz(r0));
+  }
+  // the first `have` of the rows at src; zeros past those
+  __device__ inline void request(const char* src, const uint8_t*, int have, const bf16* tile) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const bf16* dst = tile + (e * GEN_THR + 64 * wave) * 8;
+      if (r0 + RPE * e < have) {
+        lds_load16(src, off + e * RPE * 2 * D, dst);
+      } else {
+        typedef __attribute__((address_space(3))) volatile uint64_t lds_u64;
+        lds_u64* z = (lds_u64*)(dst + 8 * (threadIdx.x & 63));
+        z[0] = 0;
+        z[1] = 0;
+      }
+    }
+  }
+  __device__ inline void arrive(const bf16*) {}
+};
+
+template <int D, int T> struct GenStage<D, T, true> {
+  static constexpr int RPE = GEN_THR / (D / 8), N = T / RPE;
+  int r0, slot;
+  u32 off;
+  u32x2 code[N];
+  u32 ex[N];
+  __device__ inline GenStage(int t, int) : r0(t / (D / 8)), slot(t) {
+    off = r0 * D + 8 * ((t % (D / 8)) ^ GenTile<D>::swz(r0));
+  }
+  __device__ inline void request(const char* src, const uint8_t* exps, int have, const bf16*) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      code[e] = u32x2{0, 0};
+      ex[e] = 127;
+      if (r0 + RPE * e < have) {
+        code[e] = *reinterpret_cast<const u32x2*>(src + off + e * RPE * D);
+        ex[e] = exps[r0 + RPE * e];
+      }
+    }
+  }
+  // what was requested last, as bf16
+  __device__ inline void arrive(bf16* tile) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float f = exp_scale(ex[e]);
+      const u32x2 a = dequantise(code[e][0], f), b = dequantise(code[e][1], f);
+      typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+      *(lds_u32x4*)(tile + (e * GEN_THR + slot) * 8) = u32x4{a[0], a[1], b[0], b[1]};
+    }
+  }
+};
+
+template <int D> constexpr int gen_step() { return D == 128 ? 32 : 64; }   // keys of a step: 8 KB of a tile
+
+// Many rows: 32 of them a wave, every step's keys through LDS for all four.
+template <int D, bool E4M3>
+__device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, int lane,
+                                bf16* __restrict__ lds) {
+  constexpr int T = gen_step<D>(), NS = D / 32, DT = D / 16, TILE = T * D, ROWB = E4M3 ? D : 2 * D;
+  typedef GenTile<D> L;
+  const CacheView& c = A.c;
+  const int seg = it[GI_SEG], group = A.Hq / c.H, m = it[GI_N];
+  const int g = lane >> 4, i = lane & 15;
+  const Reach reach(c, seg, it[GI_NEW]);
+  const int32_t n = reach.n;
+  // (as in gen_few; lo of the tile, so that all waves go over to the masked steps together)
+  const int32_t lo = reach.of(it[GI_ROW] / group), most = reach.of((it[GI_ROW] + m - 1) / group);
+  const int32_t hi = 32 * wave < m ? reach.of((it[GI_ROW] + min(32 * wave + 32, m) - 1) / group) : 0;
+  int32_t from, end;
+  split_steps<T>(it, most, from, end);
+
+  const Scalars table = scalars(c.pages) + static_cast<int64_t>(seg) * c.pitch;
+  GenStage<D, T, E4M3> sk(threadIdx.x, wave), sv(threadIdx.x, wave);
+  const auto request = [&](int32_t u, bf16* tile) {
+    const int32_t key0 = u * T, p = table[key0 / GEN_PAGE], part = key0 % GEN_PAGE;
+    const int have = p >= 0 && p < c.n_pages ? n - key0 : 0;
+    const int64_t b = (static_cast<int64_t>(have > 0 ? p : 0) * c.H + hk) * GEN_PAGE + part;
+    sk.request(c.k + b * ROWB, c.ke + b, have, tile);
+    sv.request(c.v + b * ROWB, c.ve + b, have, tile + TILE);
+  };
+  if (from < end) request(from, lds);
+
+  // stacked row of column i of half a (padding rows repeat the last one), and its place
+  const auto stacked_of = [&](int a) { return it[GI_ROW] + min(32 * wave + 16 * a + i, m - 1); };
+  bf16x8 qf[2][NS];
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    const int r = stacked_of(a);
+    const int64_t row = A.order[it[GI_FIRST] + r / group], head = hk * group + r % group;
+    const bf16* qp = A.q + (row * A.Hq + head) * D + 8 * g;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[a][s] = *reinterpret_cast<const bf16x8*>(qp + 32 * s);
+  }
+  RowState<DT> st[2];
+  st[0].clear();
+  st[1].clear();
+  bool odds = false;
+
+  if constexpr (E4M3) {
+    if (from < end) {
+      sk.arrive(lds);
+      sv.arrive(lds + TILE);
+      if (from + 1 < end) request(from + 1, nullptr);
+    }
+  }
+  // One step; `edge`: some key may be hidden from some row of the tile.
+  const auto step = [&](int32_t u, auto edge_) {
+    constexpr bool edge = decltype(edge_)::value;
+    const int32_t key0 = u * T, buf = (u - from) & 1;
+    bf16 *tk = lds + 2 * buf * TILE, *tv = tk + TILE, *next = lds + 2 * (buf ^ 1) * TILE;
+    if constexpr (E4M3) {
+      __syncthreads();                       // this step's tiles are here, the other pair's readers are done
+      if (u + 1 < end) {
+        sk.arrive(next);
+        sv.arrive(next + TILE);
+        if (u + 2 < end) request(u + 2, nullptr);
+      }
+    } else {
+      lds_landed();
+      if (u + 1 < end) request(u + 1, next);
+    }
+    const int32_t page = table[key0 / GEN_PAGE];
+    if (key0 >= hi || page < 0 || page >= c.n_pages) return;   // (the same for the whole wave)
+    f32x4 s[2][T / 16];
+#pragma unroll
+    for (int j = 0; j < T / 16; ++j) s[0][j] = s[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    __builtin_amdgcn_s_setprio(1);           // the SIMD's other waves do their softmax meanwhile
+#pragma unroll
+    for (int d = 0; d < NS; ++d)
+#pragma unroll
+      for (int j = 0; j < T / 16; ++j) {
+        const bf16x8 kf = L::rows(tk, 16 * j, d, lane);
+        s[0][j] = mfma32(kf, qf[0][d], s[0][j]);
+        s[1][j] = mfma32(kf, qf[1][d], s[1][j]);
+      }
+    __builtin_amdgcn_s_setprio(0);
+    float top[2];
+    bool up = false;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      top[a] = -INFINITY;
+      const int32_t lim = edge ? reach.of(stacked_of(a) / group) : 0;
+#pragma unroll
+      for (int j = 0; j < T / 16; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[a][j][e] *= A.scale;
+          if (edge && key0 + 16 * j + 4 * g + e >= lim) s[a][j][e] = -INFINITY;
+          top[a] = fmaxf(top[a], s[a][j][e]);
+        }
+      up |= top[a] > st[a].ref + GEN_SLACK;
+    }
+    if (__any(up)) {
+      st[0].raise(top[0]);
+      st[1].raise(top[1]);
+    }
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      const float r = st[a].zero_point();
+#pragma unroll
+      for (int j = 0; j < T / 16; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[a][j][e] = __builtin_amdgcn_exp2f(s[a][j][e] - r);
+          st[a].sum += s[a][j][e];
+        }
+    }
+    u32 odd = 0;
+#pragma unroll
+    for (int h = 0; h < T / 32; ++h) {
+      bf16x8 w[2];
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        const f32x4 &x = s[a][2 * h], &y = s[a][2 * h + 1];
+        w[a] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]),
+                                                pack_bf16(y[2], y[3])});
+      }
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int j = 0; j < DT; ++j) {
+        bf16x8 vf = L::columns(tv, 32 * h, 16 * j, lane);
+        if constexpr (edge) {
+          u32x4 f = __builtin_bit_cast(u32x4, vf);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) f[e] = finite_pair(f[e], odd);
+          vf = __builtin_bit_cast(bf16x8, f);
+        }
+        st[0].acc[j] = mfma32(vf, w[0], st[0].acc[j]);
+        st[1].acc[j] = mfma32(vf, w[1], st[1].acc[j]);
+        if constexpr (edge) __builtin_amdgcn_sched_barrier(0);   // (one fragment's registers at a time)
+      }
+      __builtin_amdgcn_s_setprio(0);
+    }
+    if constexpr (edge) odds |= __any(odd != 0);
+  };
+  const int32_t mid = min(end, max(from, lo / T));
+  for (int32_t u = from; u < mid; ++u) step(u, std::false_type{});
+  for (int32_t u = mid; u < end; ++u) step(u, std::true_type{});
 
 #pragma unroll
-  for (int t = 0; t < T; ++t) {
-    if (!live[t]) continue;
-    const int32_t p0 = A.part_off[row[t]], parts = A.part_off[row[t] + 1] - p0;
-    const int64_t rh = static_cast<int64_t>(row[t]) * A.Hq + head[t];
+  for (int a = 0; a < 2; ++a) {
+    st[a].sum = over_groups_sum(st[a].sum);
+    if (32 * wave + 16 * a + i >= m) continue;
+    const int r = stacked_of(a), row = A.order[it[GI_FIRST] + r / group], head = hk * group + r % group;
+    const int32_t lim = reach.of(r / group);
+    const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
     if (parts == 1) {
-      const float f = sum[t] == 0.f ? 0.f : 1.f / sum[t];
-      u32 out[D / 8];
+      const int64_t rh = static_cast<int64_t>(row) * A.Hq + head;
+      const float f = st[a].sum == 0.f ? 0.f : 1.f / st[a].sum;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int j = 0; j < DT; j += 2)
-          out[e * (DT / 2) + j / 2] = pack_bf16(acc[t][j][e] * f, acc[t][j + 1][e] * f);
-      u32x4* op = reinterpret_cast<u32x4*>(A.o + rh * D + g * (D / 4));
-#pragma unroll
-      for (int e = 0; e < D / 32; ++e) op[e] = u32x4{out[4 * e], out[4 * e + 1], out[4 * e + 2], out[4 * e + 3]};
-      if (A.lse && g == 0)
-        A.lse[rh] = sum[t] == 0.f ? -INFINITY : (ref[t] + __builtin_amdgcn_logf(sum[t])) * GEN_LN2;
+      for (int j = 0; j < DT; ++j) Vec4<bf16>::store(A.o + rh * D + 16 * j + 4 * g, st[a].acc[j] * f);
+      if (A.lse && g == 0) A.lse[rh] = log_sum(st[a].ref, st[a].sum);
+      if (odds)
+        for (int32_t u = mid; u < end; ++u)
+          for (int j = 0; j < DT; ++j)
+            add_odd<D, E4M3>(c, table, hk, u * T, T, n, lim, A.o + rh * D, 16 * j + 4 * g, 4);
     } else {
-      const int64_t at = (static_cast<int64_t>(p0) + it[GI_PART] + it[GI_SPLIT]) * A.Hq + head[t];
-      f32x4* ap = reinterpret_cast<f32x4*>(A.acc + at * D + g * (D / 4));
+      const int64_t at = (static_cast<int64_t>(p0) + it[GI_PART] + it[GI_SPLIT]) * A.Hq + head;
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int j = 0; j < DT; j += 4)
-          ap[(e * DT + j) / 4] = f32x4{acc[t][j][e], acc[t][j + 1][e], acc[t][j + 2][e], acc[t][j + 3][e]};
+      for (int j = 0; j < DT; ++j) *reinterpret_cast<f32x4*>(A.acc + at * D + 16 * j + 4 * g) = st[a].acc[j];
       if (g == 0) {
-        A.ml[2 * at] = ref[t];
-        A.ml[2 * at + 1] = sum[t];
+        A.ml[2 * at] = st[a].ref;
+        A.ml[2 * at + 1] = st[a].sum;
       }
+      if (odds)
+        for (int32_t u = mid; u < end; ++u)
+          for (int j = 0; j < DT; ++j)
+            add_odd<D, E4M3>(c, table, hk, u * T, T, n, lim, A.acc + at * D, 16 * j + 4 * g, 4);
     }
   }
 }
 
 template <int D, bool E4M3>
-__global__ __launch_bounds__(GEN_THR, 2) void k_gen_attn(GenArgs A) {
-  __shared__ float lds[2 * join_floats<D, 2>()];
+__global__ __launch_bounds__(GEN_THR, 3) void k_gen_attn(GenArgs A) {
+  constexpr int TILES = 4 * gen_step<D>() * D * 2;   // bytes of two pairs of tiles
+  static_assert(TILES >= 2 * 64 * GEN_JOIN * 4, "a join fits");
+  __shared__ __align__(16) char lds[TILES];
   const int item = blockIdx.x / A.c.H, hk = blockIdx.x % A.c.H;
-  const int32_t* it = A.items + static_cast<int64_t>(item) * GI_WORDS;
+  const Scalars it = scalars(A.items) + static_cast<int64_t>(item) * GI_WORDS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int tiles = it[GI_TILES];
-  if (tiles == 1) gen_item<D, E4M3, 1>(A, it, hk, wave, lane, lds);
-  else gen_item<D, E4M3, 2>(A, it, hk, wave, lane, lds);
+  if (it[GI_TILES] == 1) gen_few<D, E4M3>(A, it, hk, wave, lane, reinterpret_cast<float*>(lds));
+  else gen_many<D, E4M3>(A, it, hk, wave, lane, reinterpret_cast<bf16*>(lds));
 }
 
 // One wave per (row, query head) of several parts: maxima and sums of up to 64
@@ -652,7 +936,7 @@ __global__ __launch_bounds__(GEN_THR) void k_gen_join(GenArgs A, int64_t n) {
   bf16* op = A.o + rh * D + lane * W;
 #pragma unroll
   for (int e = 0; e < W; ++e) op[e] = static_cast<bf16>(acc[e] * f);
-  if (A.lse && lane == 0) A.lse[rh] = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * GEN_LN2;
+  if (A.lse && lane == 0) A.lse[rh] = log_sum(ref, sum);
 }
 
 int gen_status(const char* where) {

@@ -20,7 +20,7 @@ enum GenItem : int {
   GI_NEW = 6,     // the segment's own new rows (the first of its rows in `order`)
   GI_PART = 7,    // a row's first part in the segment
   GI_TILES = 8,   // 16-row tiles of a wave: 1 or 2
-  GI_WAVES = 9,   // waves along the rows: 1, 2 or 4; the others share the keys
+  GI_WAVES = 9,   // waves along the rows: 1, 2 or 4; where fewer than 4, the others share the keys
   GI_WORDS = 12
 };
 

@@ -33,13 +33,13 @@ struct GenPlan {
   harts_gen_sizes sz{};
 };
 
-// Row tiles of a wave and waves along the rows for a stack of m rows: as few
-// padded rows as the kernel's shapes allow; past 128 rows, tiles of 128.
+// How an item takes a stack of m rows: up to 32 with waves that share the keys
+// (16 rows a wave, one or two waves along the rows), past that in tiles of 128
+// rows whose four waves step through the keys together.
 struct Shape { int32_t tiles, waves; };
 Shape shape_of(int64_t m) {
   if (m <= 16) return {1, 1};
-  if (m <= 32) return {2, 1};
-  if (m <= 64) return {2, 2};
+  if (m <= 32) return {1, 2};
   return {2, 4};
 }
 
