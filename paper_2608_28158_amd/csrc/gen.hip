@@ -436,7 +436,7 @@ __device__ inline void add_odd(const CacheView& c, Scalars table, int hk, int32_
 
 constexpr int GEN_JOIN = 35;   // floats a lane leaves in LDS for a join at D = 128
 
-// Few rows: 16 of them a wave; GI_WAVES waves along the rows, the others share
+// Few rows: 16 of them a wave; one, two or four (GI_WAVES) waves along the rows, the others share
 // the keys.
 template <int D, bool E4M3>
 __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, int lane,
@@ -456,6 +456,7 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
   const bool live = local < it[GI_N];
   const int stacked = it[GI_ROW] + (live ? local : 0), place = stacked / group;
   const int32_t row = A.order[it[GI_FIRST] + place], head = hk * group + stacked % group;
+  const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
   int32_t lim = reach.of(place);
   bf16x8 qf[D / 32];
   const bf16* qp = A.q + (static_cast<int64_t>(row) * A.Hq + head) * D;
@@ -572,7 +573,6 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
   }
   if (kw != 0 || !live) return;
 
-  const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
   if (parts == 1) {
     const int64_t rh = static_cast<int64_t>(row) * A.Hq + head;
     const float f = st.sum == 0.f ? 0.f : 1.f / st.sum;
@@ -662,38 +662,42 @@ template <int D, int T> struct GenStage<D, T, false> {
       }
     }
   }
-  __device__ inline void arrive(const bf16*) {}
 };
 
+// 8-bit rows land as they are in a buffer of LDS, 16 codes a lane, from where
+// the lane that requested them takes them to the tile as bf16: nothing but two
+// scale exponents waits in registers while a step computes (with the codes
+// there too, 25 registers were spilled: 65k keys, 256 rows, 8 heads 142 us).
 template <int D, int T> struct GenStage<D, T, true> {
-  static constexpr int RPE = GEN_THR / (D / 8), N = T / RPE;
-  int r0, slot;
-  u32 off;
-  u32x2 code[N];
-  u32 ex[N];
-  __device__ inline GenStage(int t, int) : r0(t / (D / 8)), slot(t) {
-    off = r0 * D + 8 * ((t % (D / 8)) ^ GenTile<D>::swz(r0));
+  static constexpr int LPR = D / 16;         // lanes of a row
+  static_assert(T * LPR == GEN_THR, "one request a tile");
+  int r, wave, slot0, slot1;
+  u32 off, ex;
+  __device__ inline GenStage(int t, int wave_) : r(t / LPR), wave(wave_), off(16 * t) {
+    const int p = 2 * (t % LPR), x = GenTile<D>::swz(r);
+    slot0 = r * (D / 8) + (p ^ x);
+    slot1 = r * (D / 8) + ((p + 1) ^ x);
   }
-  __device__ inline void request(const char* src, const uint8_t* exps, int have, const bf16*) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      code[e] = u32x2{0, 0};
-      ex[e] = 127;
-      if (r0 + RPE * e < have) {
-        code[e] = *reinterpret_cast<const u32x2*>(src + off + e * RPE * D);
-        ex[e] = exps[r0 + RPE * e];
-      }
+  __device__ inline void request(const char* src, const uint8_t* exps, int have, const char* raw) {
+    ex = 0;                                  // (a row past `have`: its codes are whatever was there)
+    if (r < have) {
+      lds_load16(src, off, raw + 1024 * wave);
+      ex = exps[r];
     }
   }
-  // what was requested last, as bf16
-  __device__ inline void arrive(bf16* tile) {
+  // after the wave's requests have landed
+  __device__ inline void arrive(const char* raw, bf16* tile) {
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    const u32x4 x = *(const lds_u32x4*)(raw + off);
+    const float f = exp_scale(ex);
+    u32x4 y[2];
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float f = exp_scale(ex[e]);
-      const u32x2 a = dequantise(code[e][0], f), b = dequantise(code[e][1], f);
-      typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
-      *(lds_u32x4*)(tile + (e * GEN_THR + slot) * 8) = u32x4{a[0], a[1], b[0], b[1]};
+    for (int h = 0; h < 2; ++h) {
+      const u32x2 a = dequantise(x[2 * h], f), b = dequantise(x[2 * h + 1], f);
+      y[h] = ex == 0 ? u32x4{0, 0, 0, 0} : u32x4{a[0], a[1], b[0], b[1]};
     }
+    *(lds_u32x4*)(tile + slot0 * 8) = y[0];
+    *(lds_u32x4*)(tile + slot1 * 8) = y[1];
   }
 };
 
@@ -718,12 +722,31 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
 
   const Scalars table = scalars(c.pages) + static_cast<int64_t>(seg) * c.pitch;
   GenStage<D, T, E4M3> sk(threadIdx.x, wave), sv(threadIdx.x, wave);
+  // the keys and values of step u on their way: bf16 to `tile`, 8-bit to the buffer behind the tiles
+  char* raw = reinterpret_cast<char*>(lds + 4 * TILE);
   const auto request = [&](int32_t u, bf16* tile) {
     const int32_t key0 = u * T, p = table[key0 / GEN_PAGE], part = key0 % GEN_PAGE;
     const int have = p >= 0 && p < c.n_pages ? n - key0 : 0;
     const int64_t b = (static_cast<int64_t>(have > 0 ? p : 0) * c.H + hk) * GEN_PAGE + part;
-    sk.request(c.k + b * ROWB, c.ke + b, have, tile);
-    sv.request(c.v + b * ROWB, c.ve + b, have, tile + TILE);
+    if constexpr (E4M3) {
+      sk.request(c.k + b * ROWB, c.ke + b, have, raw);
+      sv.request(c.v + b * ROWB, c.ve + b, have, raw + TILE);
+    } else {
+      sk.request(c.k + b * ROWB, nullptr, have, tile);
+      sv.request(c.v + b * ROWB, nullptr, have, tile + TILE);
+    }
+  };
+  // 8-bit rows of the step requested last, from the buffer to `tile`; the next ones' turn
+  const auto arrive = [&](int32_t u, bf16* tile) {
+    if constexpr (E4M3) {
+      __builtin_amdgcn_s_waitcnt(0x0f70);    // the wave's loads have landed (vmcnt 0)
+      asm volatile("" ::: "memory");
+      sk.arrive(raw, tile);
+      sv.arrive(raw + TILE, tile + TILE);
+      __builtin_amdgcn_s_waitcnt(0xc07f);    // and been read (lgkmcnt 0) before others land on them
+      asm volatile("" ::: "memory");
+      if (u + 1 < end) request(u + 1, nullptr);
+    }
   };
   if (from < end) request(from, lds);
 
@@ -743,13 +766,7 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
   st[1].clear();
   bool odds = false;
 
-  if constexpr (E4M3) {
-    if (from < end) {
-      sk.arrive(lds);
-      sv.arrive(lds + TILE);
-      if (from + 1 < end) request(from + 1, nullptr);
-    }
-  }
+  if (from < end) arrive(from, lds);
   // One step; `edge`: some key may be hidden from some row of the tile.
   const auto step = [&](int32_t u, auto edge_) {
     constexpr bool edge = decltype(edge_)::value;
@@ -757,11 +774,7 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
     bf16 *tk = lds + 2 * buf * TILE, *tv = tk + TILE, *next = lds + 2 * (buf ^ 1) * TILE;
     if constexpr (E4M3) {
       __syncthreads();                       // this step's tiles are here, the other pair's readers are done
-      if (u + 1 < end) {
-        sk.arrive(next);
-        sv.arrive(next + TILE);
-        if (u + 2 < end) request(u + 2, nullptr);
-      }
+      if (u + 1 < end) arrive(u + 1, next);
     } else {
       lds_landed();
       if (u + 1 < end) request(u + 1, next);
@@ -879,9 +892,9 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
 
 template <int D, bool E4M3>
 __global__ __launch_bounds__(GEN_THR, 3) void k_gen_attn(GenArgs A) {
-  constexpr int TILES = 4 * gen_step<D>() * D * 2;   // bytes of two pairs of tiles
-  static_assert(TILES >= 2 * 64 * GEN_JOIN * 4, "a join fits");
-  __shared__ __align__(16) char lds[TILES];
+  constexpr int TILE = gen_step<D>() * D * 2;      // bytes
+  static_assert(4 * TILE >= 2 * 64 * GEN_JOIN * 4, "a join fits");
+  __shared__ __align__(16) char lds[E4M3 ? 5 * TILE : 4 * TILE];
   const int item = blockIdx.x / A.c.H, hk = blockIdx.x % A.c.H;
   const Scalars it = scalars(A.items) + static_cast<int64_t>(item) * GI_WORDS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -889,54 +902,76 @@ __global__ __launch_bounds__(GEN_THR, 3) void k_gen_attn(GenArgs A) {
   else gen_many<D, E4M3>(A, it, hk, wave, lane, reinterpret_cast<bf16*>(lds));
 }
 
-// One wave per (row, query head) of several parts: maxima and sums of up to 64
-// parts in the lanes, then the accumulators, D / 64 columns a lane.
-template <int D>
+// Joins the parts of (row, query head) entries that have several.  D / 4 lanes
+// hold a part's accumulators, four columns each; SUBS such groups take an
+// entry's parts in turn, each with a reference of its own, and meet in LDS.
+// With many parts an entry has the whole workgroup, or their reads, one after
+// the other, would set the time (96 parts of 16 rows x 32 heads: 40 us with one
+// wave an entry, 8 so).
+template <int D, int SUBS>
 __global__ __launch_bounds__(GEN_THR) void k_gen_join(GenArgs A, int64_t n) {
-  constexpr int W = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int64_t rh = static_cast<int64_t>(blockIdx.x) * (GEN_THR / 64) + (threadIdx.x >> 6);
-  if (rh >= n) return;
-  const int32_t row = static_cast<int32_t>(rh / A.Hq), head = static_cast<int32_t>(rh % A.Hq);
-  const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
-  if (parts == 1) return;
-  float ref = -INFINITY, sum = 0.f, acc[W];
-#pragma unroll
-  for (int e = 0; e < W; ++e) acc[e] = 0.f;
-  for (int b = 0; b < parts; b += 64) {
-    const int m = min(64, parts - b);
-    float r1 = -INFINITY, s1 = 0.f;
-    if (lane < m) {
-      const float* ml = A.ml + 2 * ((static_cast<int64_t>(p0) + b + lane) * A.Hq + head);
-      r1 = ml[0];
-      s1 = ml[1];
-    }
-    float to = fmaxf(ref, r1);
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) to = fmaxf(to, __shfl_xor(to, s));
+  constexpr int LPG = D / 4, ENTRIES = GEN_THR / LPG / SUBS, U = 4;
+  const int t = threadIdx.x, c = 4 * (t % LPG), grp = t / LPG, sub = grp % SUBS;
+  const int64_t rh = static_cast<int64_t>(blockIdx.x) * ENTRIES + grp / SUBS;
+  int32_t p0 = 0, parts = 0, head = 0;
+  if (rh < n) {
+    const int32_t row = static_cast<int32_t>(rh / A.Hq);
+    head = static_cast<int32_t>(rh % A.Hq);
+    p0 = A.part_off[row];
+    parts = A.part_off[row + 1] - p0;
+  }
+  float ref = -INFINITY, sum = 0.f;
+  f32x4 acc{0.f, 0.f, 0.f, 0.f};
+  const auto add = [&](float to, float s1, float r1, const f32x4& x) {
     const float r = to == -INFINITY ? 0.f : to;
-    const float f0 = __builtin_amdgcn_exp2f(ref - r), f1 = __builtin_amdgcn_exp2f(r1 - r);
-    float add = lane < m ? s1 * f1 : 0.f;
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) add += __shfl_xor(add, s);
-    sum = sum * f0 + add;
+    const float f = __builtin_amdgcn_exp2f(r1 - r);
+    sum += s1 * f;
+    acc += x * f;
+  };
+  const auto rise = [&](float to) {
+    const float f = to == ref ? 1.f : __builtin_amdgcn_exp2f(ref - to);
     ref = to;
+    sum *= f;
+    acc *= f;
+  };
+  for (int b = sub; b < parts; b += U * SUBS) {
+    float r1[U], s1[U];
+    f32x4 x[U];
 #pragma unroll
-    for (int e = 0; e < W; ++e) acc[e] *= f0;
-    const float* ap = A.acc + ((static_cast<int64_t>(p0) + b) * A.Hq + head) * D + lane * W;
-#pragma unroll 4
-    for (int p = 0; p < m; ++p) {
-      const float f = __shfl(f1, p);
-      const float* x = ap + static_cast<int64_t>(p) * A.Hq * D;
+    for (int k = 0; k < U; ++k) {
+      const int p = b + k * SUBS;
+      r1[k] = -INFINITY;
+      s1[k] = 0.f;
+      x[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (p < parts) {
+        const int64_t at = (static_cast<int64_t>(p0) + p) * A.Hq + head;
+        r1[k] = A.ml[2 * at];
+        s1[k] = A.ml[2 * at + 1];
+        x[k] = *reinterpret_cast<const f32x4*>(A.acc + at * D + c);
+      }
+    }
+    rise(fmaxf(fmaxf(fmaxf(ref, r1[0]), fmaxf(r1[1], r1[2])), r1[3]));
 #pragma unroll
-      for (int e = 0; e < W; ++e) acc[e] += x[e] * f;
+    for (int k = 0; k < U; ++k) add(ref, s1[k], r1[k], x[k]);
+  }
+  if constexpr (SUBS > 1) {
+    __shared__ f32x4 sx[GEN_THR];
+    __shared__ float sr[GEN_THR / LPG], ss[GEN_THR / LPG];
+    sx[t] = acc;
+    if (t % LPG == 0) {
+      sr[grp] = ref;
+      ss[grp] = sum;
+    }
+    __syncthreads();
+    if (sub != 0) return;
+    for (int k = 1; k < SUBS; ++k) {
+      rise(fmaxf(ref, sr[grp + k]));
+      add(ref, ss[grp + k], sr[grp + k], sx[t + k * LPG]);
     }
   }
-  const float f = sum == 0.f ? 0.f : 1.f / sum;
-  bf16* op = A.o + rh * D + lane * W;
-#pragma unroll
-  for (int e = 0; e < W; ++e) op[e] = static_cast<bf16>(acc[e] * f);
-  if (A.lse && lane == 0) A.lse[rh] = log_sum(ref, sum);
+  if (parts <= 1) return;
+  Vec4<bf16>::store(A.o + rh * D + c, acc * (sum == 0.f ? 0.f : 1.f / sum));
+  if (A.lse && c == 0) A.lse[rh] = log_sum(ref, sum);
 }
 
 int gen_status(const char* where) {
@@ -1083,9 +1118,20 @@ extern "C" int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* s
   if (int rc = gen_status("k_gen_attn")) return rc;
   if (sizes->n_join > 0) {
     const int64_t n = sizes->n_rows * Hq;
-    const uint32_t blocks = static_cast<uint32_t>((n + GEN_THR / 64 - 1) / (GEN_THR / 64));
-    if (cache->d == 128) hipLaunchKernelGGL(k_gen_join<128>, dim3(blocks), dim3(GEN_THR), 0, s, A, n);
-    else hipLaunchKernelGGL(k_gen_join<64>, dim3(blocks), dim3(GEN_THR), 0, s, A, n);
+    // groups of an entry by its parts, on average
+    const int64_t parts = sizes->n_parts / sizes->n_rows;
+    const auto join = [&](auto kernel, int64_t entries) {
+      hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>((n + entries - 1) / entries)), dim3(GEN_THR), 0, s, A, n);
+    };
+    if (cache->d == 128) {
+      if (parts >= 32) join(k_gen_join<128, 8>, 1);
+      else if (parts >= 8) join(k_gen_join<128, 4>, 2);
+      else join(k_gen_join<128, 1>, 8);
+    } else {
+      if (parts >= 32) join(k_gen_join<64, 16>, 1);
+      else if (parts >= 8) join(k_gen_join<64, 4>, 4);
+      else join(k_gen_join<64, 1>, 16);
+    }
     return gen_status("k_gen_join");
   }
   return HARTS_OK;

@@ -24,10 +24,24 @@ enum GenItem : int {
   GI_WORDS = 12
 };
 
-// A split is as long as leaves GEN_FILL workgroups, and at least GEN_MIN_SPLIT
-// keys.
-constexpr int64_t GEN_FILL = 768;
-constexpr int64_t GEN_MIN_SPLIT = 512;
+// How long segments are split.  The chip holds GEN_SLOTS workgroups at once
+// (three on each of 256 CUs).  While a fair share of a call's keys per slot is
+// below GEN_ROUND, a split is that share, lengthened by up to 2 until all
+// workgroups run in one round (a second one, of few, would double the time:
+// 1,000 new rows of 1,000, 4 key heads 47 us in 1,024 workgroups, 35 in 672), but
+// no shorter than GEN_MIN_SPLIT keys nor, up to GEN_ALONE keys, so short that a
+// segment has more than GEN_FEW_PARTS parts, whose join would cost more than
+// the shorter splits save (one row of 3,000 keys, 16 heads: 13.5 us in 24
+// parts, 11.4 in 12).  Past that, splits are shares of one and a half rounds,
+// which balances items of unequal weight (64 rows of 65k keys and 64 tails:
+// 165 us at one round, 148).  A call whose rows each see one segment of at most
+// GEN_ALONE keys is not split at all and needs no join (333 keys, 16 heads: 9.1 us
+// in one launch, 9.6 in two, and the second launch is the host's time too).
+constexpr int64_t GEN_SLOTS = 768;
+constexpr int64_t GEN_ROUND = 1024;
+constexpr int64_t GEN_MIN_SPLIT = 128;
+constexpr int64_t GEN_FEW_PARTS = 16;
+constexpr int64_t GEN_ALONE = 512;
 constexpr int64_t GEN_MAX_SPLITS = 4096;
 
 }  // namespace harts

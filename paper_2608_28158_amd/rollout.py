@@ -40,25 +40,25 @@ def _device(device):
     return d if d.index is not None else torch.device("cuda", torch.cuda.current_device())
 
 
-class _on:
-    """The library launches on the current device: the tensors' one."""
+# The current stream's handle without a Stream object around it (0.1 us instead
+# of 1.2, of a small call's 7), where torch offers that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    def __init__(self, device):
-        self.index = device.index
 
-    def __enter__(self):
-        self.was = torch.cuda.current_device()
-        if self.was != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream(self.index).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.was != self.index:
-            torch.cuda.set_device(self.was)
+def _call(index, what, fn, *args):
+    """fn(*args, stream) on the tensors' device: the library launches on the current one."""
+    if torch.cuda.current_device() == index:
+        code = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            code = fn(*args, _raw_stream(index))
+    if code:
+        _lib.check(code, what)
 
 
 def _check(name, t, shape, dtype, device):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
@@ -96,8 +96,9 @@ class RolloutCache:
         self._held = [[] for _ in range(n_seg)]
         code = _lib.HARTS_BF16 if kind == "bf16" else _lib.HARTS_E4M3
         ptr = lambda t, i: None if t is None else t[i].data_ptr()
-        self._desc = [_lib.Cache(ptr(self.k, i), ptr(self.v, i), ptr(self.k_exp, i), ptr(self.v_exp, i),
-                                 self.pages.data_ptr(), self.len.data_ptr(), n_pages, n_seg, pitch, heads, d, code)
+        fixed = (self.pages.data_ptr(), self.len.data_ptr(), n_pages, n_seg, pitch, heads, d, code)
+        # (the library's view of each layer: the tensors above are written, never replaced)
+        self._desc = [C.byref(_lib.Cache(*(ptr(t, i) for t in (self.k, self.v, self.k_exp, self.v_exp)), *fixed))
                       for i in range(layers)]
 
     # -- pages (host bookkeeping) --------------------------------------------
@@ -137,7 +138,7 @@ class RolloutCache:
     def desc(self, layer: int):
         if not 0 <= layer < self.layers:
             raise ValueError(f"layer {layer} outside [0, {self.layers})")
-        return C.byref(self._desc[layer])
+        return self._desc[layer]
 
     def write(self, rows, k, v, layer: int = 0):
         """Rows k, v [n, heads, d] (bf16) into the cache at ``rows`` [n, 2]
@@ -145,11 +146,11 @@ class RolloutCache:
         may be named once; entries that name no existing row are skipped."""
         n = rows.shape[0]
         _check("rows", rows, (n, 2), torch.int32, self.device)
-        _check("k", k, (n, self.heads, self.d), torch.bfloat16, self.device)
-        _check("v", v, (n, self.heads, self.d), torch.bfloat16, self.device)
-        with _on(self.device) as stream:
-            _lib.check(self.L.harts_cache_write(self.desc(layer), rows.data_ptr(), n, k.data_ptr(), v.data_ptr(),
-                                                stream), "harts_cache_write")
+        shape = (n, self.heads, self.d)
+        _check("k", k, shape, torch.bfloat16, self.device)
+        _check("v", v, shape, torch.bfloat16, self.device)
+        _call(self.device.index, "harts_cache_write", self.L.harts_cache_write, self.desc(layer), rows.data_ptr(), n,
+              k.data_ptr(), v.data_ptr())
 
     def read(self, rows, layer: int = 0):
         """(k, v) [n, heads, d] bf16: what the rows stand for, zeros where an
@@ -158,9 +159,8 @@ class RolloutCache:
         _check("rows", rows, (n, 2), torch.int32, self.device)
         k = torch.empty((n, self.heads, self.d), dtype=torch.bfloat16, device=self.device)
         v = torch.empty_like(k)
-        with _on(self.device) as stream:
-            _lib.check(self.L.harts_cache_read(self.desc(layer), rows.data_ptr(), n, k.data_ptr(), v.data_ptr(),
-                                               stream), "harts_cache_read")
+        _call(self.device.index, "harts_cache_read", self.L.harts_cache_read, self.desc(layer), rows.data_ptr(), n,
+              k.data_ptr(), v.data_ptr())
         return k, v
 
 
@@ -196,6 +196,9 @@ class RolloutBatch:
         _lib.check(self.L.harts_gen_workspace_size(C.byref(self.sizes), self.q_heads, cache.d, C.byref(size)),
                    "harts_gen_workspace_size")
         self.ws_bytes = size.value
+        self._shape = torch.Size((self.n_rows, self.q_heads, cache.d))
+        self._tables = (C.byref(self.sizes), self._items.data_ptr(), self._order.data_ptr(), self._off.data_ptr(),
+                        self.q_heads)
 
     def advance(self):
         """The segments' lengths grow by their new rows."""
@@ -209,32 +212,34 @@ class RolloutBatch:
         """(o [n_rows, q_heads, d] bf16, lse [n_rows, q_heads] float32) of the
         new rows' queries; scale defaults to d ** -0.5."""
         c = self.cache
-        shape = (self.n_rows, self.q_heads, c.d)
-        _check("q", q, shape, torch.bfloat16, c.device)
+        _check("q", q, self._shape, torch.bfloat16, c.device)
         if out is None:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=c.device)
+            out = torch.empty_like(q)
         else:
-            _check("out", out, shape, torch.bfloat16, c.device)
-        lse = torch.empty(shape[:2], dtype=torch.float32, device=c.device)
+            _check("out", out, self._shape, torch.bfloat16, c.device)
+        lse = torch.empty(self._shape[:2], dtype=torch.float32, device=c.device)
         # (from the allocator at every call: calls on other streams, or captured into other graphs, share none)
-        ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=c.device)
-        with _on(c.device) as stream:
-            _lib.check(self.L.harts_gen_attn(c.desc(layer), C.byref(self.sizes), self._items.data_ptr(),
-                                             self._order.data_ptr(), self._off.data_ptr(), self.q_heads,
-                                             float(c.d ** -0.5 if scale is None else scale), q.data_ptr(),
-                                             out.data_ptr(), lse.data_ptr(), ws.data_ptr(), self.ws_bytes, stream),
-                       "harts_gen_attn")
+        ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=c.device).data_ptr() if self.ws_bytes else None
+        _call(c.device.index, "harts_gen_attn", self.L.harts_gen_attn, c.desc(layer), *self._tables,
+              c.d ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(), lse.data_ptr(), ws, self.ws_bytes)
         return out, lse
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _step(kda, q, k, v, g, beta, S, S_out, idx_in, idx_out, row_off, scale, out):
     if q.dim() != 3 or q.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("q must be float32 or bfloat16 [rows, H, d]")
-    n_rows, H, d = q.shape
-    dev = _device(q.device)
-    for name, t in (("q", q), ("k", k), ("v", v)):
-        _check(name, t, (n_rows, H, d), q.dtype, dev)
-    _check("g", g, (n_rows, H, d) if kda else (n_rows, H), torch.float32, dev)
+    if not q.is_cuda:
+        raise RuntimeError("generation runs on the GPU only")
+    n_rows, H, d = shape = q.shape
+    dev = q.device
+    _check("q", q, shape, q.dtype, dev)
+    _check("k", k, shape, q.dtype, dev)
+    _check("v", v, shape, q.dtype, dev)
+    _check("g", g, shape if kda else shape[:2], torch.float32, dev)
     if kda:
         _check("beta", beta, (n_rows, H), torch.float32, dev)
     if row_off is not None:
@@ -246,8 +251,10 @@ def _step(kda, q, k, v, g, beta, S, S_out, idx_in, idx_out, row_off, scale, out)
         if idx_out is not None:
             raise ValueError("an update in place leaves every state where it was: idx_out has to be None")
         S_out, idx_out = S, idx_in
-    for name, t, idx in (("S", S, idx_in), ("S_out", S_out, idx_out)):
-        _check(name, t, (t.shape[0], H, d, d), torch.float32, dev)
+    elif S_out is S and idx_out is not idx_in:
+        raise ValueError("an update in place leaves every state where it was: S_out and idx_out have to be None")
+    for name, t, idx in (("S", S, idx_in), ("S_out", S_out, idx_out))[:1 if S_out is S else 2]:
+        _check(name, t, t.shape[:1] + (H, d, d), torch.float32, dev)
         if idx is not None:
             _check("index of " + name, idx, (n_seq,), torch.int32, dev)
         elif t.shape[0] < n_seq:
@@ -256,15 +263,16 @@ def _step(kda, q, k, v, g, beta, S, S_out, idx_in, idx_out, row_off, scale, out)
         out = torch.empty_like(q)
     else:
         _check("out", out, q.shape, q.dtype, dev)
-    L, ptr = _lib.lib(), lambda t: None if t is None else t.data_ptr()
-    code = _lib.HARTS_F32 if q.dtype == torch.float32 else _lib.HARTS_BF16
-    head = (code, n_seq, n_rows, H, d, float(d ** -0.5 if scale is None else scale), ptr(q), ptr(k), ptr(v), ptr(g))
-    tail = (ptr(row_off), ptr(S), ptr(idx_in), S.shape[0], ptr(S_out), ptr(idx_out), S_out.shape[0], ptr(out))
-    with _on(dev) as stream:
-        if kda:
-            _lib.check(L.harts_kda_step(*head, ptr(beta), *tail, stream), "harts_kda_step")
-        else:
-            _lib.check(L.harts_la_step(*head, *tail, stream), "harts_la_step")
+    L, ptr = _lib.lib(), _ptr
+    code = _lib.HARTS_F32 if q.dtype is torch.float32 else _lib.HARTS_BF16
+    head = (code, n_seq, n_rows, H, d, d ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(),
+            v.data_ptr(), g.data_ptr())
+    tail = (ptr(row_off), S.data_ptr(), ptr(idx_in), S.shape[0], S_out.data_ptr(), ptr(idx_out), S_out.shape[0],
+            out.data_ptr())
+    if kda:
+        _call(dev.index, "harts_kda_step", L.harts_kda_step, *head, beta.data_ptr(), *tail)
+    else:
+        _call(dev.index, "harts_la_step", L.harts_la_step, *head, *tail)
     return out
 
 

@@ -232,8 +232,10 @@ def test_refusals():
             call(False, x, **kw)
     with pytest.raises(RuntimeError):
         call(False, {**x, "v": x["v"].cuda().requires_grad_()}, S=S)
-    with pytest.raises(_lib.HartsError):
+    with pytest.raises(ValueError):
         call(False, x, S=S, S_out=S, idx_out=ints([1, 0]))
+    with pytest.raises(_lib.HartsError):
+        call(False, x, S=S, S_out=S.view(2, 2, 64, 64), idx_out=ints([1, 0]))
     v = x["v"].cuda()
     with pytest.raises(_lib.HartsError):
         call(False, {**x, "v": v}, S=S, out=v)
