@@ -19,7 +19,7 @@
 //
 // Few rows (gen_few): the item is bound by reading the keys and values, so
 // nothing stands between memory and the products.  A wave has 16 rows and every
-// second or fourth 32-key step, straight from the cache into registers, with no
+// second or fourth step of 32 or 64 keys, straight from the cache into registers, with no
 // LDS and no barrier in the loop; the next step is requested as soon as this
 // one's registers are free, and the waves join through LDS at the end.
 //   - V^T fragments need 8 keys of one column per lane.  A lane reads 8 rows'
@@ -242,12 +242,10 @@ template <int D> struct KvStep<D, false> {
     }
   }
   __device__ inline bf16x8 k_frag(int t, int s) const { return __builtin_bit_cast(bf16x8, k[t][s]); }
-  // the lane's columns of its 8 keys as bf16 pairs
-  __device__ inline void v_rows(u32 (&w)[8][VW]) const {
+  // columns 2q, 2q + 1 of the lane's, of its 8 keys, as bf16 pairs
+  __device__ inline void v_pairs(u32 (&w)[8], int q) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int i = 0; i < VW; ++i) w[e][i] = v[e][i];
+    for (int e = 0; e < 8; ++e) w[e] = v[e][q];
   }
 };
 
@@ -293,27 +291,23 @@ template <int D> struct KvStep<D, true> {
     const u32x2 a = dequantise(x[2 * (s & 1)], f), b = dequantise(x[2 * (s & 1) + 1], f);
     return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
   }
-  __device__ inline void v_rows(u32 (&w)[8][VW]) const {
+  __device__ inline void v_pairs(u32 (&w)[8], int q) const {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float f = exp_scale((vs[e >> 2] >> (8 * (e & 3))) & 0xffu);
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) {
-        const u32x2 a = dequantise(v[e][i], f);
-        w[e][2 * i] = a[0];
-        w[e][2 * i + 1] = a[1];
-      }
+      const bf16x2 x = (q & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e][q >> 1], f, true)
+                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[e][q >> 1], f, false);
+      w[e] = __builtin_bit_cast(u32, x);
     }
   }
 };
 
-// Column j of the lane's 8 rows of pairs as one fragment.
-template <int VW>
-__device__ inline bf16x8 v_frag(const u32 (&w)[8][VW], int j) {
+// The first or second column of the lane's 8 pairs as one fragment.
+__device__ inline bf16x8 v_frag(const u32 (&w)[8], int second) {
   u32x4 f;
 #pragma unroll
   for (int p = 0; p < 4; ++p)
-    f[p] = __builtin_amdgcn_perm(w[2 * p + 1][j >> 1], w[2 * p][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
+    f[p] = __builtin_amdgcn_perm(w[2 * p + 1], w[2 * p], second ? 0x07060302u : 0x05040100u);
   return __builtin_bit_cast(bf16x8, f);
 }
 
@@ -336,11 +330,17 @@ struct GenArgs {
   CacheView c;
   const int32_t *items, *order, *part_off;
   int32_t Hq;
-  float scale;                 // scale * log2(e)
+  float scale;                 // |scale| * log2(e)
+  u32 sign;                    // 0x80008000 where the scale is negative: q's signs change instead, so
+                               // that the largest product is the largest score
   const bf16* q;
   bf16* o;
   float *lse, *acc, *ml;       // acc [parts][Hq][D], ml [parts][Hq][2]
 };
+
+__device__ inline bf16x8 q_frag(const GenArgs& A, const bf16* p) {
+  return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p) ^ A.sign);
+}
 
 // What an item's rows see: rows of the segment that exist (n), all that were
 // written or are to come (cached), its own new rows.
@@ -436,12 +436,15 @@ __device__ inline void add_odd(const CacheView& c, Scalars table, int hk, int32_
 
 constexpr int GEN_JOIN = 35;   // floats a lane leaves in LDS for a join at D = 128
 
-// Few rows: 16 of them a wave; one, two or four (GI_WAVES) waves along the rows, the others share
-// the keys.
+// Few rows: 16 of them a wave; one, two or four (GI_WAVES) waves along the rows,
+// the others share the keys.
 template <int D, bool E4M3>
 __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, int lane,
                                float* __restrict__ lds) {
   typedef KvStep<D, E4M3> Step;
+  // keys of a step: 32, or 64 of 64 bytes each, for as many bytes on the way (at
+  // D = 128, 64 8-bit keys spill: 64 rows of 2,000 keys, 8 heads 111 us against 63)
+  constexpr int NK = E4M3 && D == 64 ? 2 : 1, T = 32 * NK;
   constexpr int DT = D / 16;                        // 16-column tiles
   static_assert(3 + 4 * DT <= GEN_JOIN, "room for a join");
   const CacheView& c = A.c;
@@ -461,7 +464,7 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
   bf16x8 qf[D / 32];
   const bf16* qp = A.q + (static_cast<int64_t>(row) * A.Hq + head) * D;
 #pragma unroll
-  for (int s = 0; s < D / 32; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + Step::k_col(s, g));
+  for (int s = 0; s < D / 32; ++s) qf[s] = q_frag(A, qp + Step::k_col(s, g));
   // the fewest and the most keys that a row of the wave sees: places grow along
   // it, and what a row sees with its place (own rows one more each, then the
   // descendants', which see all)
@@ -471,75 +474,92 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
   if (!live) lim = n;                               // padding rows take part and are dropped
 
   int32_t from, end;
-  split_steps<32>(it, hi, from, end);
+  split_steps<T>(it, hi, from, end);
   RowState<DT> st;
   st.clear();
   bool odds = false;
 
   const Scalars table = scalars(c.pages) + static_cast<int64_t>(seg) * c.pitch;
   const auto page_of = [&](int32_t u) {
-    const int32_t p = table[u >> 1];
+    const int32_t p = table[u * T / GEN_PAGE];
     return p >= 0 && p < c.n_pages ? p : -1;
   };
   const auto base_of = [&](int32_t page) {
     return (static_cast<int64_t>(page < 0 ? 0 : page) * c.H + hk) * GEN_PAGE;
   };
-  Step x;
+  Step x[NK];
+  const auto load_k = [&](int32_t u, int64_t b) {
+#pragma unroll
+    for (int h = 0; h < NK; ++h) x[h].load_k(c.k + b * Step::ROWB, c.ke + b, (u * NK + h) & 1, lane);
+  };
+  const auto load_v = [&](int32_t u, int64_t b) {
+#pragma unroll
+    for (int h = 0; h < NK; ++h) x[h].load_v(c.v + b * Step::ROWB, c.ve + b, (u * NK + h) & 1, lane);
+  };
   int32_t u = from + kw, page = -1;
   if (u < end) {
     page = page_of(u);
     const int64_t b = base_of(page);
-    x.load_k(c.k + b * Step::ROWB, c.ke + b, u & 1, lane);
-    x.load_v(c.v + b * Step::ROWB, c.ve + b, u & 1, lane);
+    load_k(u, b);
+    load_v(u, b);
   }
   for (; u < end; u += kws) {
-    const int32_t key0 = u * 32;
-    const bool more = u + kws < end;
-    const int32_t next = more ? page_of(u + kws) : page;
+    const int32_t key0 = u * T, next_u = u + kws;
+    const bool more = next_u < end;
+    const int32_t next = more ? page_of(next_u) : -1;
     const int64_t nb = base_of(next);
-    const int nhalf = (more ? u + kws : u) & 1;
 
-    f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+    f32x4 s[2 * NK];
 #pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
+    for (int t = 0; t < 2 * NK; ++t) {
+      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int d = 0; d < D / 32; ++d) s[kt] = mfma32(x.k_frag(kt, d), qf[d], s[kt]);
-    x.load_k(c.k + nb * Step::ROWB, c.ke + nb, nhalf, lane);
+      for (int d = 0; d < D / 32; ++d) s[t] = mfma32(x[t / 2].k_frag(t & 1, d), qf[d], s[t]);
+    }
+    if (more) load_k(next_u, nb);
 
-    const bool edge = key0 + 32 > lo || page < 0;   // some key is hidden from some row
-    float y[8], top = -INFINITY;
+    const bool edge = key0 + T > lo || page < 0;    // some key is hidden from some row
+    float y[8 * NK], top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      y[e] = s[e >> 2][e & 3] * A.scale;
-      if (edge && (key0 + frag_key(g, e) >= lim || page < 0)) y[e] = -INFINITY;
+    for (int e = 0; e < 8 * NK; ++e) {
+      y[e] = s[e >> 2][e & 3];
+      if (edge && (key0 + 32 * (e / 8) + frag_key(g, e % 8) >= lim || page < 0)) y[e] = -INFINITY;
       top = fmaxf(top, y[e]);
     }
+    top *= A.scale;
     if (__any(top > st.ref + GEN_SLACK)) st.raise(top);
     const float r = st.zero_point();
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      y[e] = __builtin_amdgcn_exp2f(y[e] - r);
+    for (int e = 0; e < 8 * NK; ++e) {
+      y[e] = __builtin_amdgcn_exp2f(fmaf(y[e], A.scale, -r));
+      // (with a scale of 0 too)
+      if (edge && (key0 + 32 * (e / 8) + frag_key(g, e % 8) >= lim || page < 0)) y[e] = 0.f;
       st.sum += y[e];
     }
-    const bf16x8 w = __builtin_bit_cast(
-        bf16x8, u32x4{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])});
-
-    u32 vw[8][Step::VW];
-    x.v_rows(vw);
-    if (edge) {
-      // (rows that do not exist hold anything)
-      u32 odd = 0;
+    u32 odd = 0;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool there = page >= 0 && key0 + frag_key(g, e) < n;
+    for (int h = 0; h < NK; ++h) {
+      const float* z = y + 8 * h;
+      const bf16x8 w = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(z[0], z[1]), pack_bf16(z[2], z[3]),
+                                                        pack_bf16(z[4], z[5]), pack_bf16(z[6], z[7])});
 #pragma unroll
-        for (int q = 0; q < Step::VW; ++q) vw[e][q] = there ? finite_pair(vw[e][q], odd) : 0u;
+      for (int q = 0; q < Step::VW; ++q) {
+        u32 vw[8];
+        x[h].v_pairs(vw, q);
+        if (edge) {
+          // (rows that do not exist hold anything)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const bool there = page >= 0 && key0 + 32 * h + frag_key(g, e) < n;
+            vw[e] = there ? finite_pair(vw[e], odd) : 0u;
+          }
+        }
+        st.acc[2 * q] = mfma32(v_frag(vw, 0), w, st.acc[2 * q]);
+        st.acc[2 * q + 1] = mfma32(v_frag(vw, 1), w, st.acc[2 * q + 1]);
       }
-      odds |= __any(odd != 0);
     }
-#pragma unroll
-    for (int j = 0; j < DT; ++j) st.acc[j] = mfma32(v_frag(vw, j), w, st.acc[j]);
-    x.load_v(c.v + nb * Step::ROWB, c.ve + nb, nhalf, lane);
+    if (edge) odds |= __any(odd != 0);
+    if (more) load_v(next_u, nb);
     page = next;
   }
   st.sum = over_groups_sum(st.sum);
@@ -587,8 +607,8 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
     for (int e = 0; e < D / 32; ++e) op[e] = u32x4{out[4 * e], out[4 * e + 1], out[4 * e + 2], out[4 * e + 3]};
     if (A.lse && g == 0) A.lse[rh] = log_sum(st.ref, st.sum);
     if (odds)
-      for (u = max(from, lo / 32); u < end; ++u)
-        add_odd<D, E4M3>(c, table, hk, u * 32, 32, n, lim, A.o + rh * D, g * (D / 4), D / 4);
+      for (u = max(from, lo / T); u < end; ++u)
+        add_odd<D, E4M3>(c, table, hk, u * T, T, n, lim, A.o + rh * D, g * (D / 4), D / 4);
   } else {
     const int64_t at = (static_cast<int64_t>(p0) + it[GI_PART] + it[GI_SPLIT]) * A.Hq + head;
     f32x4* ap = reinterpret_cast<f32x4*>(A.acc + at * D + g * (D / 4));
@@ -602,8 +622,8 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
       A.ml[2 * at + 1] = st.sum;
     }
     if (odds)
-      for (u = max(from, lo / 32); u < end; ++u)
-        add_odd<D, E4M3>(c, table, hk, u * 32, 32, n, lim, A.acc + at * D, g * (D / 4), D / 4);
+      for (u = max(from, lo / T); u < end; ++u)
+        add_odd<D, E4M3>(c, table, hk, u * T, T, n, lim, A.acc + at * D, g * (D / 4), D / 4);
   }
 }
 
@@ -671,12 +691,15 @@ template <int D, int T> struct GenStage<D, T, false> {
 template <int D, int T> struct GenStage<D, T, true> {
   static constexpr int LPR = D / 16;         // lanes of a row
   static_assert(T * LPR == GEN_THR, "one request a tile");
-  int r, wave, slot0, slot1;
+  int r, wave, swap, slot0, slot1;
   u32 off, ex;
   __device__ inline GenStage(int t, int wave_) : r(t / LPR), wave(wave_), off(16 * t) {
+    // (odd lanes take the second piece first: a write of 16 lanes then fills all
+    // banks once, where even pieces alone would take each second one twice)
     const int p = 2 * (t % LPR), x = GenTile<D>::swz(r);
-    slot0 = r * (D / 8) + (p ^ x);
-    slot1 = r * (D / 8) + ((p + 1) ^ x);
+    swap = t & 1;
+    slot0 = r * (D / 8) + ((p + swap) ^ x);
+    slot1 = r * (D / 8) + ((p + 1 - swap) ^ x);
   }
   __device__ inline void request(const char* src, const uint8_t* exps, int have, const char* raw) {
     ex = 0;                                  // (a row past `have`: its codes are whatever was there)
@@ -693,7 +716,8 @@ template <int D, int T> struct GenStage<D, T, true> {
     u32x4 y[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const u32x2 a = dequantise(x[2 * h], f), b = dequantise(x[2 * h + 1], f);
+      const int second = h ^ swap;
+      const u32x2 a = dequantise(second ? x[2] : x[0], f), b = dequantise(second ? x[3] : x[1], f);
       y[h] = ex == 0 ? u32x4{0, 0, 0, 0} : u32x4{a[0], a[1], b[0], b[1]};
     }
     *(lds_u32x4*)(tile + slot0 * 8) = y[0];
@@ -759,7 +783,7 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
     const int64_t row = A.order[it[GI_FIRST] + r / group], head = hk * group + r % group;
     const bf16* qp = A.q + (row * A.Hq + head) * D + 8 * g;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[a][s] = *reinterpret_cast<const bf16x8*>(qp + 32 * s);
+    for (int s = 0; s < NS; ++s) qf[a][s] = q_frag(A, qp + 32 * s);
   }
   RowState<DT> st[2];
   st[0].clear();
@@ -794,20 +818,20 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
         s[1][j] = mfma32(kf, qf[1][d], s[1][j]);
       }
     __builtin_amdgcn_s_setprio(0);
+    const int32_t lim[2] = {edge ? reach.of(stacked_of(0) / group) : 0, edge ? reach.of(stacked_of(1) / group) : 0};
     float top[2];
     bool up = false;
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
       top[a] = -INFINITY;
-      const int32_t lim = edge ? reach.of(stacked_of(a) / group) : 0;
 #pragma unroll
       for (int j = 0; j < T / 16; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s[a][j][e] *= A.scale;
-          if (edge && key0 + 16 * j + 4 * g + e >= lim) s[a][j][e] = -INFINITY;
+          if (edge && key0 + 16 * j + 4 * g + e >= lim[a]) s[a][j][e] = -INFINITY;
           top[a] = fmaxf(top[a], s[a][j][e]);
         }
+      top[a] *= A.scale;
       up |= top[a] > st[a].ref + GEN_SLACK;
     }
     if (__any(up)) {
@@ -821,7 +845,8 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
       for (int j = 0; j < T / 16; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s[a][j][e] = __builtin_amdgcn_exp2f(s[a][j][e] - r);
+          s[a][j][e] = __builtin_amdgcn_exp2f(fmaf(s[a][j][e], A.scale, -r));
+          if (edge && key0 + 16 * j + 4 * g + e >= lim[a]) s[a][j][e] = 0.f;   // (with a scale of 0 too)
           st[a].sum += s[a][j][e];
         }
     }
@@ -1102,7 +1127,8 @@ extern "C" int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* s
   A.order = order;
   A.part_off = part_off;
   A.Hq = Hq;
-  A.scale = scale * GEN_LOG2E;
+  A.scale = fabsf(scale) * GEN_LOG2E;
+  A.sign = scale < 0.f ? 0x80008000u : 0u;
   A.q = static_cast<const bf16*>(q);
   A.o = static_cast<bf16*>(o);
   A.lse = lse;

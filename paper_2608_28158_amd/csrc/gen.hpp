@@ -32,9 +32,10 @@ enum GenItem : int {
 // no shorter than GEN_MIN_SPLIT keys nor, up to GEN_ALONE keys, so short that a
 // segment has more than GEN_FEW_PARTS parts, whose join would cost more than
 // the shorter splits save (one row of 3,000 keys, 16 heads: 13.5 us in 24
-// parts, 11.4 in 12).  Past that, splits are shares of one and a half rounds,
-// which balances items of unequal weight (64 rows of 65k keys and 64 tails:
-// 165 us at one round, 148).  A call whose rows each see one segment of at most
+// parts, 11.4 in 12).  Past that, splits are such shares where the workgroups
+// then fit one round (256 rows of 65k keys, 8 heads: 113 us, 125 in one and a
+// half), else shares of one and a half rounds, which balances items of unequal
+// weight (with 64 tails of 2,000 keys: 165 us at one round, 148 so).  A call whose rows each see one segment of at most
 // GEN_ALONE keys is not split at all and needs no join (333 keys, 16 heads: 9.1 us
 // in one launch, 9.6 in two, and the second launch is the host's time too).
 constexpr int64_t GEN_SLOTS = 768;

@@ -33,16 +33,18 @@ struct GenPlan {
   harts_gen_sizes sz{};
 };
 
-// How an item takes a stack of m rows: up to 64 with 16 rows a wave, one, two or
-// four waves along the rows, the others sharing the keys; past that in tiles of
-// 128 rows whose four waves step through the keys together.  (Up to 64: a tile
-// would be half empty, 31 samples of 2 rows after a 282-row prompt 14.2 us
-// against 11.8.)
+// How an item takes a stack of m rows of a segment of `cap` keys: up to 32 with
+// 16 rows a wave, one or two waves along the rows, the others sharing the keys;
+// past that in tiles of 128 rows whose four waves step through the keys
+// together.  33 to 64 rows of a short segment, where latency counts, have four
+// waves along the rows (31 samples of 2 rows after a 282-row prompt: 14.2 us in
+// half-empty tiles, 11.8 so), but those of a long one do not, as each wave reads
+// all keys (64 rows of 65k keys, 8 heads: 115 us against 80).
 struct Shape { int32_t tiles, waves; };
-Shape shape_of(int64_t m) {
+Shape shape_of(int64_t m, int64_t cap) {
   if (m <= 16) return {1, 1};
   if (m <= 32) return {1, 2};
-  if (m <= 64) return {1, 4};
+  if (m <= 64 && cap <= GEN_ALONE) return {1, 4};
   return {2, 4};
 }
 
@@ -94,17 +96,17 @@ int make(const char* where, int32_t n_seg, const int32_t* parent, const int32_t*
   }
   const auto tiles_of = [&](int32_t s) {
     const int64_t m = P.below[s] * group;
-    const Shape f = shape_of(m);
+    const Shape f = shape_of(m, cap[s]);
     return ceil_div(m, int64_t{16} * f.tiles * f.waves);
   };
   // keys of a split (gen.hpp says why)
   const auto splits_of = [&](int32_t s, int64_t len) {
     return std::max<int64_t>(1, std::min<int64_t>(ceil_div(cap[s], len), GEN_MAX_SPLITS));
   };
-  const auto workgroups = [&](int64_t len) {
+  const auto workgroups = [&](int64_t len) {         // (without the very short ones)
     int64_t n = 0;
     for (int32_t s = 0; s < n_seg; ++s)
-      if (P.below[s] > 0) n += tiles_of(s) * splits_of(s, len) * Hkv;
+      if (P.below[s] > 0 && cap[s] >= len / 8) n += tiles_of(s) * splits_of(s, len) * Hkv;
     return n;
   };
   double total = 0;
@@ -121,7 +123,9 @@ int make(const char* where, int32_t n_seg, const int32_t* parent, const int32_t*
   if (alone) {
     L = GEN_ALONE;
   } else if (L >= GEN_ROUND) {
-    L = std::max(GEN_ROUND, share(GEN_SLOTS * 3 / 2));
+    int64_t i = 0;
+    while (i <= 2 && workgroups(L * (16 + i) / 16) > GEN_SLOTS) ++i;
+    L = i <= 2 ? L * (16 + i) / 16 : std::max(GEN_ROUND, share(GEN_SLOTS * 3 / 2));
   } else {
     L = std::max({L, GEN_MIN_SPLIT, std::min(GEN_ALONE, longest / GEN_FEW_PARTS)});
     const int64_t least = L;
@@ -201,7 +205,7 @@ extern "C" int harts_gen_tables(int32_t n_seg, const int32_t* parent, const int3
     for (const int32_t s : P.preorder) {
       const int64_t m = P.below[s] * group;
       if (m == 0) continue;
-      const Shape f = shape_of(m);
+      const Shape f = shape_of(m, cap[s]);
       const int64_t tile = int64_t{16} * f.tiles * f.waves, keys = ceil_div(cap[s], P.splits[s]);
       for (int32_t c = 0; c < P.splits[s]; ++c)
         for (int64_t r = 0; r < m; r += tile)
@@ -211,7 +215,7 @@ extern "C" int harts_gen_tables(int32_t n_seg, const int32_t* parent, const int3
     std::stable_sort(list.begin(), list.end(), [](const Item& a, const Item& b) { return a.work > b.work; });
     int32_t* w = items;
     for (const Item& it : list) {
-      const Shape f = shape_of(P.below[it.seg] * group);
+      const Shape f = shape_of(P.below[it.seg] * group, cap[it.seg]);
       w[GI_SEG] = it.seg;
       w[GI_FIRST] = static_cast<int32_t>(P.start[it.seg]);
       w[GI_ROW] = static_cast<int32_t>(it.row);

@@ -40,15 +40,17 @@ def _device(device):
     return d if d.index is not None else torch.device("cuda", torch.cuda.current_device())
 
 
-# The current stream's handle without a Stream object around it (0.1 us instead
-# of 1.2, of a small call's 7), where torch offers that.
+# The current stream's handle and device without the objects and the lazy
+# initialisation around them (0.2 us instead of 1.4, of a small call's 7), where
+# torch offers that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call(index, what, fn, *args):
     """fn(*args, stream) on the tensors' device: the library launches on the current one."""
-    if torch.cuda.current_device() == index:
+    if _current() == index:
         code = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
@@ -57,13 +59,22 @@ def _call(index, what, fn, *args):
         _lib.check(code, what)
 
 
-def _check(name, t, shape, dtype, device):
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.requires_grad and torch.is_grad_enabled():
-        raise RuntimeError(f"{name} requires a gradient; generation is not differentiable")
+def _check(shape, dtype, device, names, *tensors):
+    """Contiguous tensors of one shape, type and device, none of them recording a gradient."""
+    for t in tensors:
+        if (t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != device or
+                t.requires_grad):
+            break
+    else:
+        return
+    for name, t in zip(names.split(), tensors):
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}"
+                             f"{'' if t.is_contiguous() else ' with strides ' + str(t.stride())}")
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, expected {device}")
+        if t.requires_grad and torch.is_grad_enabled():
+            raise RuntimeError(f"{name} requires a gradient; generation is not differentiable")
 
 
 class RolloutCache:
@@ -145,10 +156,8 @@ class RolloutCache:
         (int32 segment and position, negative from the segment's end).  A row
         may be named once; entries that name no existing row are skipped."""
         n = rows.shape[0]
-        _check("rows", rows, (n, 2), torch.int32, self.device)
-        shape = (n, self.heads, self.d)
-        _check("k", k, shape, torch.bfloat16, self.device)
-        _check("v", v, shape, torch.bfloat16, self.device)
+        _check((n, 2), torch.int32, self.device, "rows", rows)
+        _check((n, self.heads, self.d), torch.bfloat16, self.device, "k v", k, v)
         _call(self.device.index, "harts_cache_write", self.L.harts_cache_write, self.desc(layer), rows.data_ptr(), n,
               k.data_ptr(), v.data_ptr())
 
@@ -156,7 +165,7 @@ class RolloutCache:
         """(k, v) [n, heads, d] bf16: what the rows stand for, zeros where an
         entry names no existing row."""
         n = rows.shape[0]
-        _check("rows", rows, (n, 2), torch.int32, self.device)
+        _check((n, 2), torch.int32, self.device, "rows", rows)
         k = torch.empty((n, self.heads, self.d), dtype=torch.bfloat16, device=self.device)
         v = torch.empty_like(k)
         _call(self.device.index, "harts_cache_read", self.L.harts_cache_read, self.desc(layer), rows.data_ptr(), n,
@@ -212,11 +221,11 @@ class RolloutBatch:
         """(o [n_rows, q_heads, d] bf16, lse [n_rows, q_heads] float32) of the
         new rows' queries; scale defaults to d ** -0.5."""
         c = self.cache
-        _check("q", q, self._shape, torch.bfloat16, c.device)
+        _check(self._shape, torch.bfloat16, c.device, "q", q)
         if out is None:
             out = torch.empty_like(q)
         else:
-            _check("out", out, self._shape, torch.bfloat16, c.device)
+            _check(self._shape, torch.bfloat16, c.device, "out", out)
         lse = torch.empty(self._shape[:2], dtype=torch.float32, device=c.device)
         # (from the allocator at every call: calls on other streams, or captured into other graphs, share none)
         ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=c.device).data_ptr() if self.ws_bytes else None
@@ -230,45 +239,45 @@ def _ptr(t):
 
 
 def _step(kda, q, k, v, g, beta, S, S_out, idx_in, idx_out, row_off, scale, out):
-    if q.dim() != 3 or q.dtype not in (torch.float32, torch.bfloat16):
+    shape, dtype, dev = q.shape, q.dtype, q.device
+    if len(shape) != 3 or (dtype is not torch.bfloat16 and dtype is not torch.float32):
         raise ValueError("q must be float32 or bfloat16 [rows, H, d]")
-    if not q.is_cuda:
+    if dev.type != "cuda":
         raise RuntimeError("generation runs on the GPU only")
-    n_rows, H, d = shape = q.shape
-    dev = q.device
-    _check("q", q, shape, q.dtype, dev)
-    _check("k", k, shape, q.dtype, dev)
-    _check("v", v, shape, q.dtype, dev)
-    _check("g", g, shape if kda else shape[:2], torch.float32, dev)
+    n_rows, H, d = shape
+    if out is None:
+        _check(shape, dtype, dev, "q k v", q, k, v)
+        out = torch.empty_like(q)
+    else:
+        _check(shape, dtype, dev, "q k v out", q, k, v, out)
+    _check(shape if kda else (n_rows, H), torch.float32, dev, "g", g)
     if kda:
-        _check("beta", beta, (n_rows, H), torch.float32, dev)
+        _check((n_rows, H), torch.float32, dev, "beta", beta)
+    n_seq = n_rows
     if row_off is not None:
-        _check("row_off", row_off, (row_off.numel(),), torch.int32, dev)
-        if row_off.numel() < 1:
+        n_seq = row_off.numel() - 1
+        if n_seq < 0:
             raise ValueError("row_off has one entry more than there are sequences")
-    n_seq = n_rows if row_off is None else row_off.numel() - 1
+        _check((n_seq + 1,), torch.int32, dev, "row_off", row_off)
     if S_out is None:
         if idx_out is not None:
             raise ValueError("an update in place leaves every state where it was: idx_out has to be None")
         S_out, idx_out = S, idx_in
     elif S_out is S and idx_out is not idx_in:
         raise ValueError("an update in place leaves every state where it was: S_out and idx_out have to be None")
-    for name, t, idx in (("S", S, idx_in), ("S_out", S_out, idx_out))[:1 if S_out is S else 2]:
-        _check(name, t, t.shape[:1] + (H, d, d), torch.float32, dev)
+    n_in, n_out = len(S), len(S_out)
+    _check((n_in, H, d, d), torch.float32, dev, "S", S)
+    if S_out is not S:
+        _check((n_out, H, d, d), torch.float32, dev, "S_out", S_out)
+    for idx, n, name in ((idx_in, n_in, "S"), (idx_out, n_out, "S_out")):
         if idx is not None:
-            _check("index of " + name, idx, (n_seq,), torch.int32, dev)
-        elif t.shape[0] < n_seq:
-            raise ValueError(f"{name} has {t.shape[0]} states for {n_seq} sequences and no index")
-    if out is None:
-        out = torch.empty_like(q)
-    else:
-        _check("out", out, q.shape, q.dtype, dev)
-    L, ptr = _lib.lib(), _ptr
-    code = _lib.HARTS_F32 if q.dtype is torch.float32 else _lib.HARTS_BF16
-    head = (code, n_seq, n_rows, H, d, d ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(),
-            v.data_ptr(), g.data_ptr())
-    tail = (ptr(row_off), S.data_ptr(), ptr(idx_in), S.shape[0], S_out.data_ptr(), ptr(idx_out), S_out.shape[0],
-            out.data_ptr())
+            _check((n_seq,), torch.int32, dev, "index", idx)
+        elif n < n_seq:
+            raise ValueError(f"{name} has {n} states for {n_seq} sequences and no index")
+    L = _lib.lib()
+    head = (_lib.HARTS_BF16 if dtype is torch.bfloat16 else _lib.HARTS_F32, n_seq, n_rows, H, d,
+            d ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr())
+    tail = (_ptr(row_off), S.data_ptr(), _ptr(idx_in), n_in, S_out.data_ptr(), _ptr(idx_out), n_out, out.data_ptr())
     if kda:
         _call(dev.index, "harts_kda_step", L.harts_kda_step, *head, beta.data_ptr(), *tail)
     else:
