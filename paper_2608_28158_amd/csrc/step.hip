@@ -18,6 +18,7 @@
 
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "harts.h"
 #include "la_common.hpp"
@@ -72,16 +73,24 @@ struct Token {
   }
 };
 
-// Sum over the 8 row groups of a wave, in every lane.
-__device__ inline f32x4 over_rows(f32x4 x) {
-#pragma unroll
-  for (int s = 8; s < 64; s *= 2)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], s);
-  return x;
+// Sum over the 8 row groups of a wave (lanes 8, 16 and 32 apart), in every lane,
+// by moves between vector registers: a token's chain of dependent steps has two
+// of these, and through LDS each exchange takes ten times as long.
+__device__ inline float over_rows(float x) {
+  typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+  const auto bits = [](float y) { return __builtin_bit_cast(unsigned int, y); };
+  const auto val = [](unsigned int y) { return __builtin_bit_cast(float, y); };
+  x += val(__builtin_amdgcn_update_dpp(0u, bits(x), 0x128, 0xf, 0xf, true));   // rotate by 8 within 16 lanes
+  u32x2 p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(bits(x), bits(x), false, false));
+  x = val(p[0]) + val(p[1]);
+  p = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(bits(x), bits(x), false, false));
+  return val(p[0]) + val(p[1]);
+}
+__device__ inline f32x4 over_rows(const f32x4& x) {
+  return f32x4{over_rows(x[0]), over_rows(x[1]), over_rows(x[2]), over_rows(x[3])};
 }
 
-template <typename T, int D, bool KDA>
+template <typename T, int D, bool KDA, bool NT>
 __global__ __launch_bounds__(ST_THR) void k_step(StepArgs A) {
   constexpr int NR = D / 8, SLABS = D / ST_COLS;
   const int lane = threadIdx.x & 63;
@@ -109,7 +118,10 @@ __global__ __launch_bounds__(ST_THR) void k_step(StepArgs A) {
   if (src >= 0) {
     const float* p = A.S_in + (src * A.H + h) * (D * D) + cell;
 #pragma unroll
-    for (int i = 0; i < NR; ++i) S[i] = *reinterpret_cast<const f32x4*>(p + i * D);
+    for (int i = 0; i < NR; ++i) {
+      const f32x4* x = reinterpret_cast<const f32x4*>(p + i * D);
+      S[i] = NT ? __builtin_nontemporal_load(x) : *x;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < NR; ++i) S[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -136,25 +148,28 @@ __global__ __launch_bounds__(ST_THR) void k_step(StepArgs A) {
     if (row + 1 < end) x.load(A, row + 1, h, col, r);
     f32x4 v = Vec4Raw<T>::widen(y.v), o{0.f, 0.f, 0.f, 0.f};
     if constexpr (KDA) {
+      // o = S_t^T q = D^T q + beta (k.q) (v - D^T k): the sums that v waits for
+      // and those of o run together
       f32x4 u{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < NR / 4; ++i) {
-        const f32x4 k = Vec4Raw<T>::widen(y.k[i]);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          S[4 * i + e] *= expf(y.g[i][e]);
-          u += S[4 * i + e] * k[e];
-        }
-      }
-      v = (v - over_rows(u)) * y.beta;
+      float kq = 0.f;
 #pragma unroll
       for (int i = 0; i < NR / 4; ++i) {
         const f32x4 k = Vec4Raw<T>::widen(y.k[i]), q = Vec4Raw<T>::widen(y.q[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          S[4 * i + e] += v * k[e];
+          S[4 * i + e] *= __expf(y.g[i][e]);   // (16 a lane and token; relative error about |g| 2^-24)
+          u += S[4 * i + e] * k[e];
           o += S[4 * i + e] * q[e];
+          kq += k[e] * q[e];
         }
+      }
+      v = (v - over_rows(u)) * y.beta;
+      o = over_rows(o) + v * over_rows(kq);
+#pragma unroll
+      for (int i = 0; i < NR / 4; ++i) {
+        const f32x4 k = Vec4Raw<T>::widen(y.k[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[4 * i + e] += v * k[e];
       }
     } else {
       const float a = expf(y.g1);
@@ -167,15 +182,20 @@ __global__ __launch_bounds__(ST_THR) void k_step(StepArgs A) {
           o += S[4 * i + e] * q[e];
         }
       }
+      o = over_rows(o);
     }
-    o = over_rows(o) * A.scale;
+    o *= A.scale;
     if (r == 0) Vec4<T>::store(static_cast<T*>(A.o) + (row * A.H + h) * D + col, o);
   }
 
   if (dst >= 0) {
     float* p = A.S_out + (dst * A.H + h) * (D * D) + cell;
 #pragma unroll
-    for (int i = 0; i < NR; ++i) *reinterpret_cast<f32x4*>(p + i * D) = S[i];
+    for (int i = 0; i < NR; ++i) {
+      f32x4* x = reinterpret_cast<f32x4*>(p + i * D);
+      if (NT) __builtin_nontemporal_store(S[i], x);
+      else *x = S[i];
+    }
   }
 }
 
@@ -212,11 +232,22 @@ int step(const char* where, int32_t dtype, int32_t d, const StepArgs& A, void* s
   }
   const int64_t blocks = (A.n_seq * A.H * (d / ST_COLS) + ST_THR / 64 - 1) / (ST_THR / 64);
   if (A.n_seq > INT32_MAX || blocks > INT32_MAX) return fail(HARTS_EUNSUPPORTED, "too many sequences for one call");
+  // States past what the last-level cache holds are not kept in it (512 sequences,
+  // 16 heads of 128, two pools of 512 MiB: 214 us, 198 so; 64 sequences 23, 25 so).
+  const bool nt = A.n_seq * state > (size_t{128} << 20);
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(ST_THR), 0, static_cast<hipStream_t>(stream), A);
   };
-  if (dtype == HARTS_BF16) d == 128 ? launch(k_step<bf16, 128, KDA>) : launch(k_step<bf16, 64, KDA>);
-  else d == 128 ? launch(k_step<float, 128, KDA>) : launch(k_step<float, 64, KDA>);
+  const auto pick = [&](auto type, auto dim) {
+    typedef decltype(type) T;
+    constexpr int D = decltype(dim)::value;
+    if (nt) launch(k_step<T, D, KDA, true>);
+    else launch(k_step<T, D, KDA, false>);
+  };
+  const std::integral_constant<int, 128> d128{};
+  const std::integral_constant<int, 64> d64{};
+  if (dtype == HARTS_BF16) d == 128 ? pick(bf16{}, d128) : pick(bf16{}, d64);
+  else d == 128 ? pick(float{}, d128) : pick(float{}, d64);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? HARTS_OK : fail(HARTS_EHIP, hipGetErrorString(e));
 }
