@@ -132,7 +132,7 @@ __device__ inline u32x2 quantise(const u32x4& x, u32& exponent) {
 }
 
 // One lane: 8 elements of (row, head) of k, then of v.
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool NT>
 __global__ __launch_bounds__(GEN_THR) void k_cache_write(CacheView c, const int32_t* __restrict__ rows, int64_t n,
                                                          const u32x4* __restrict__ k_new,
                                                          const u32x4* __restrict__ v_new) {
@@ -143,7 +143,14 @@ __global__ __launch_bounds__(GEN_THR) void k_cache_write(CacheView c, const int3
   if (rh >= n * c.H) return;
   const int64_t r = rh / c.H;
   const int h = static_cast<int>(rh - r * c.H);
-  const u32x4 a = k_new[i], b = v_new[i];
+  u32x4 a, b;
+  if constexpr (!E4M3 && NT) {
+    a = __builtin_nontemporal_load(k_new + i);
+    b = __builtin_nontemporal_load(v_new + i);
+  } else {
+    a = k_new[i];
+    b = v_new[i];
+  }
   const int64_t at = cache_row(c, rows[2 * r], rows[2 * r + 1]);
   if (at < 0) return;                                // (the same for all lanes of a row)
   const int64_t slot = at + static_cast<int64_t>(h) * GEN_PAGE;
@@ -169,7 +176,7 @@ __device__ inline u32x2 dequantise(u32 w, float scale) {
   return u32x2{__builtin_bit_cast(u32, lo), __builtin_bit_cast(u32, hi)};
 }
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool NT>
 __global__ __launch_bounds__(GEN_THR) void k_cache_read(CacheView c, const int32_t* __restrict__ rows, int64_t n,
                                                         u32x4* __restrict__ k_out, u32x4* __restrict__ v_out) {
   constexpr int P = D / 8;
@@ -196,8 +203,13 @@ __global__ __launch_bounds__(GEN_THR) void k_cache_read(CacheView c, const int32
       b = reinterpret_cast<const u32x4*>(c.v)[slot * P + piece];
     }
   }
-  k_out[i] = a;
-  v_out[i] = b;
+  if constexpr (NT) {
+    __builtin_nontemporal_store(a, k_out + i);
+    __builtin_nontemporal_store(b, v_out + i);
+  } else {
+    k_out[i] = a;
+    v_out[i] = b;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -1035,11 +1047,26 @@ CacheView view_of(const harts_cache* c) {
           c->n_pages, c->n_seg, c->pitch, c->H};
 }
 
+// f(head size, whether 8-bit) of a cache, as constants
+template <typename F>
+void by_cache(const harts_cache* c, F f) {
+  const std::integral_constant<int, 128> d128{};
+  const std::integral_constant<int, 64> d64{};
+  const bool q = c->kind == HARTS_E4M3;
+  if (c->d == 128) q ? f(d128, std::true_type{}) : f(d128, std::false_type{});
+  else q ? f(d64, std::true_type{}) : f(d64, std::false_type{});
+}
+
 // blocks of a launch of one lane per 8 elements, or 0 past a grid's reach
 uint32_t piece_blocks(int64_t n, const harts_cache* c) {
   const int64_t b = (n * c->H * (c->d / 8) + GEN_THR - 1) / GEN_THR;
   return b > INT32_MAX ? 0 : static_cast<uint32_t>(b);
 }
+
+// Whether the bf16 side of a call is larger than the chip's L2 caches: it then
+// goes around them (30,000 rows x 16 heads of 128: 8-bit read 75 -> 51 us, bf16
+// write 84 -> 71; the write that quantises was no faster so, at d = 64 slower).
+bool past_l2(int64_t n, const harts_cache* c) { return n * c->H * c->d * 4 > (int64_t{32} << 20); }
 
 int check_rows(const harts_cache* c, const int32_t* rows, int64_t n, const void* k, const void* v, const char* where) {
   if (int rc = check_cache(c, where)) return rc;
@@ -1069,9 +1096,12 @@ extern "C" int harts_cache_write(const harts_cache* cache, const int32_t* rows, 
     hipLaunchKernelGGL(kernel, dim3(piece_blocks(n, cache)), dim3(GEN_THR), 0, static_cast<hipStream_t>(stream),
                        view_of(cache), rows, n, static_cast<const u32x4*>(k_new), static_cast<const u32x4*>(v_new));
   };
-  const bool q = cache->kind == HARTS_E4M3;
-  if (cache->d == 128) q ? launch(k_cache_write<128, true>) : launch(k_cache_write<128, false>);
-  else q ? launch(k_cache_write<64, true>) : launch(k_cache_write<64, false>);
+  const auto pick = [&](auto dim, auto kind) {
+    constexpr int D = decltype(dim)::value;
+    constexpr bool Q = decltype(kind)::value;
+    past_l2(n, cache) ? launch(k_cache_write<D, Q, !Q>) : launch(k_cache_write<D, Q, false>);
+  };
+  by_cache(cache, pick);
   return gen_status("k_cache_write");
 }
 
@@ -1083,9 +1113,12 @@ extern "C" int harts_cache_read(const harts_cache* cache, const int32_t* rows, i
     hipLaunchKernelGGL(kernel, dim3(piece_blocks(n, cache)), dim3(GEN_THR), 0, static_cast<hipStream_t>(stream),
                        view_of(cache), rows, n, static_cast<u32x4*>(k_out), static_cast<u32x4*>(v_out));
   };
-  const bool q = cache->kind == HARTS_E4M3;
-  if (cache->d == 128) q ? launch(k_cache_read<128, true>) : launch(k_cache_read<128, false>);
-  else q ? launch(k_cache_read<64, true>) : launch(k_cache_read<64, false>);
+  const auto pick = [&](auto dim, auto kind) {
+    constexpr int D = decltype(dim)::value;
+    constexpr bool Q = decltype(kind)::value;
+    past_l2(n, cache) ? launch(k_cache_read<D, Q, true>) : launch(k_cache_read<D, Q, false>);
+  };
+  by_cache(cache, pick);
   return gen_status("k_cache_read");
 }
 
@@ -1138,9 +1171,7 @@ extern "C" int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* s
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(sizes->n_items * cache->H)), dim3(GEN_THR), 0, s, A);
   };
-  const bool e4m3 = cache->kind == HARTS_E4M3;
-  if (cache->d == 128) e4m3 ? launch(k_gen_attn<128, true>) : launch(k_gen_attn<128, false>);
-  else e4m3 ? launch(k_gen_attn<64, true>) : launch(k_gen_attn<64, false>);
+  by_cache(cache, [&](auto dim, auto kind) { launch(k_gen_attn<decltype(dim)::value, decltype(kind)::value>); });
   if (int rc = gen_status("k_gen_attn")) return rc;
   if (sizes->n_join > 0) {
     const int64_t n = sizes->n_rows * Hq;
