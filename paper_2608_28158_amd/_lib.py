@@ -15,7 +15,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("HARTS_LIB", os.path.join(HERE, "libharts.so"))
 
 HARTS_OK, HARTS_EINVAL, HARTS_EUNSUPPORTED, HARTS_EHIP, HARTS_ENOMEM = 0, -1, -2, -3, -4
-HARTS_F32, HARTS_BF16, HARTS_E4M3 = 0, 1, 2
+HARTS_F32, HARTS_BF16 = 0, 1
+HARTS_E4M3 = 2
 
 # Every symbol include/harts.h declares.
 EXPORTS = (
@@ -29,9 +30,13 @@ EXPORTS = (
     "harts_attn_bwd", "harts_attn_scatter",
     "harts_kda_layout", "harts_kda_tables", "harts_kda_workspace_size", "harts_kda_fwd", "harts_kda_bwd",
     "harts_kda_bank_add", "harts_kda_reduce",
+    "harts_profile_begin", "harts_profile_end",
+)
+
+# Every symbol include/harts_rollout.h declares.
+ROLLOUT_EXPORTS = (
     "harts_cache_write", "harts_cache_read", "harts_gen_layout", "harts_gen_tables",
     "harts_gen_workspace_size", "harts_gen_attn", "harts_la_step", "harts_kda_step",
-    "harts_profile_begin", "harts_profile_end",
 )
 
 
@@ -217,27 +222,36 @@ def lib():
     L.harts_kda_bank_add.argtypes = [vp, i32, i32, vp, i64, vp, vp, vp]
     L.harts_kda_reduce.restype = C.c_int
     L.harts_kda_reduce.argtypes = [vp, vp, vp, i64, i64, i32, vp, vp]
-    L.harts_cache_write.restype = C.c_int
-    L.harts_cache_write.argtypes = [vp, vp, i64, vp, vp, vp]
-    L.harts_cache_read.restype = C.c_int
-    L.harts_cache_read.argtypes = [vp, vp, i64, vp, vp, vp]
-    L.harts_gen_layout.restype = C.c_int
-    L.harts_gen_layout.argtypes = [i32, vp, vp, vp, i32, i32, vp]
-    L.harts_gen_tables.restype = C.c_int
-    L.harts_gen_tables.argtypes = [i32, vp, vp, vp, i32, i32, vp, vp, vp, vp]
-    L.harts_gen_workspace_size.restype = C.c_int
-    L.harts_gen_workspace_size.argtypes = [vp, i32, i32, C.POINTER(sz)]
-    L.harts_gen_attn.restype = C.c_int
-    L.harts_gen_attn.argtypes = [vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, vp, sz, vp]
-    L.harts_la_step.restype = C.c_int
-    L.harts_la_step.argtypes = [i32, i64, i64, i32, i32, f32] + [vp] * 7 + [i64, vp, vp, i64, vp, vp]
-    L.harts_kda_step.restype = C.c_int
-    L.harts_kda_step.argtypes = [i32, i64, i64, i32, i32, f32] + [vp] * 8 + [i64, vp, vp, i64, vp, vp]
     L.harts_profile_begin.restype = C.c_int
     L.harts_profile_begin.argtypes = []
     L.harts_profile_end.restype = C.c_int
     L.harts_profile_end.argtypes = [C.POINTER(KernelTime), i32, C.POINTER(i32)]
     _lib = L
+    return L
+
+
+_rollout = None
+
+
+def rollout():
+    """The library with the generation calls (include/harts_rollout.h) declared."""
+    global _rollout
+    if _rollout is not None:
+        return _rollout
+    L = lib()
+    vp, sz, i32, i64, f32 = C.c_void_p, C.c_size_t, C.c_int32, C.c_int64, C.c_float
+    for name, args in (
+            ("harts_cache_write", [vp, vp, i64, vp, vp, vp]),
+            ("harts_cache_read", [vp, vp, i64, vp, vp, vp]),
+            ("harts_gen_layout", [i32, vp, vp, vp, i32, i32, vp]),
+            ("harts_gen_tables", [i32, vp, vp, vp, i32, i32, vp, vp, vp, vp]),
+            ("harts_gen_workspace_size", [vp, i32, i32, C.POINTER(sz)]),
+            ("harts_gen_attn", [vp, vp, vp, vp, vp, i32, f32, vp, vp, vp, vp, sz, vp]),
+            ("harts_la_step", [i32, i64, i64, i32, i32, f32] + [vp] * 7 + [i64, vp, vp, i64, vp, vp]),
+            ("harts_kda_step", [i32, i64, i64, i32, i32, f32] + [vp] * 8 + [i64, vp, vp, i64, vp, vp])):
+        fn = getattr(L, name)
+        fn.restype, fn.argtypes = C.c_int, args
+    _rollout = L
     return L
 
 

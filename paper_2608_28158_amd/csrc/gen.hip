@@ -47,7 +47,7 @@
 #include <type_traits>
 
 #include "gen.hpp"
-#include "harts.h"
+#include "harts_rollout.h"
 #include "la_common.hpp"
 #include "lds_load.hpp"
 #include "plan.hpp"
@@ -78,10 +78,10 @@ struct CacheView {
 
 // Index of (row, head 0) as page * H * 64 + slot of a row table's entry, or -1
 // if it names no existing row.
-__device__ inline int64_t cache_row(const CacheView& c, int32_t seg, int32_t pos) {
+__device__ inline int64_t cache_row(const CacheView& c, int32_t seg, int32_t entry) {
   if (seg < 0 || seg >= c.n_seg) return -1;
   const int32_t n = c.len[seg];
-  if (pos < 0) pos += n;
+  const int64_t pos = entry < 0 ? static_cast<int64_t>(n) + entry : entry;
   if (pos < 0 || pos >= n || pos / GEN_PAGE >= c.pitch) return -1;
   const int32_t page = c.pages[static_cast<int64_t>(seg) * c.pitch + pos / GEN_PAGE];
   if (page < 0 || page >= c.n_pages) return -1;
@@ -1131,8 +1131,9 @@ extern "C" int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* s
     set_error("harts_gen_attn: query heads have to be a multiple of the cache's heads, at most 65535");
     return HARTS_EUNSUPPORTED;
   }
-  if (!sizes || sizes->n_rows < 0 || sizes->n_items < 0 || sizes->n_parts < 0 || sizes->n_join < 0 ||
-      sizes->n_rows * Hq > INT32_MAX || sizes->n_items * cache->H > INT32_MAX || sizes->n_parts > INT32_MAX) {
+  const auto out_of = [](int64_t x) { return x < 0 || x > INT32_MAX; };
+  if (!sizes || out_of(sizes->n_rows) || out_of(sizes->n_items) || out_of(sizes->n_parts) || sizes->n_join < 0 ||
+      sizes->n_rows * Hq > INT32_MAX || sizes->n_items * cache->H > INT32_MAX) {
     set_error("harts_gen_attn: NULL or bad sizes");
     return HARTS_EINVAL;
   }

@@ -14,7 +14,7 @@
 #include <vector>
 
 #include "gen.hpp"
-#include "harts.h"
+#include "harts_rollout.h"
 #include "plan.hpp"
 
 using harts::set_error;

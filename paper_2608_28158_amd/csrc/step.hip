@@ -16,11 +16,12 @@
 // Everything is float32; o is rounded once.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <string>
 #include <type_traits>
 
-#include "harts.h"
+#include "harts_rollout.h"
 #include "la_common.hpp"
 #include "plan.hpp"
 
@@ -211,6 +212,8 @@ int step(const char* where, int32_t dtype, int32_t d, const StepArgs& A, void* s
   if (A.H < 1 || A.H > 65535 || (d != 64 && d != 128))
     return fail(HARTS_EUNSUPPORTED, "need 1 <= H <= 65535 and d in {64, 128}");
   if (A.n_seq < 0 || A.n_rows < 0 || A.n_in < 0 || A.n_out < 0) return fail(HARTS_EINVAL, "negative size");
+  if (std::max({A.n_seq, A.n_rows, A.n_in, A.n_out}) > INT32_MAX)
+    return fail(HARTS_EUNSUPPORTED, "more than 2^31 - 1 sequences, rows or states");
   if (A.n_seq == 0) return HARTS_OK;
   if (!A.row_off && A.n_rows < A.n_seq) return fail(HARTS_EINVAL, "fewer rows than sequences without row_off");
   if (A.n_rows > 0 && (!A.q || !A.k || !A.v || !A.g || !A.o || (KDA && !A.beta)))
@@ -231,7 +234,7 @@ int step(const char* where, int32_t dtype, int32_t d, const StepArgs& A, void* s
     if ((a < b ? b - a : a - b) < span) return fail(HARTS_EINVAL, "o overlaps an input");
   }
   const int64_t blocks = (A.n_seq * A.H * (d / ST_COLS) + ST_THR / 64 - 1) / (ST_THR / 64);
-  if (A.n_seq > INT32_MAX || blocks > INT32_MAX) return fail(HARTS_EUNSUPPORTED, "too many sequences for one call");
+  if (blocks > INT32_MAX) return fail(HARTS_EUNSUPPORTED, "too many sequences for one call");
   // States past what the last-level cache holds are not kept in it (512 sequences,
   // 16 heads of 128, two pools of 512 MiB: 214 us, 198 so; 64 sequences 23, 25 so).
   const bool nt = A.n_seq * state > (size_t{128} << 20);

@@ -90,7 +90,7 @@ class RolloutCache:
             raise ValueError("kind must be 'bf16' or 'e4m3'")
         if min(n_pages, n_seg, pitch, heads, layers) < 1 or d not in (64, 128):
             raise ValueError("need at least one page, segment, column, head and layer, and d in {64, 128}")
-        self.L, self.device = _lib.lib(), _device(device)
+        self.L, self.device = _lib.rollout(), _device(device)
         self.n_pages, self.n_seg, self.pitch, self.heads, self.d = n_pages, n_seg, pitch, heads, d
         self.kind, self.layers = kind, layers
         dt = torch.bfloat16 if kind == "bf16" else torch.float8_e4m3fn
@@ -284,7 +284,7 @@ def _step(kda, q, k, v, g, beta, S, S_out, idx_in, idx_out, row_off, scale, out)
                 _check((n_seq,), torch.int32, dev, "index", idx)
             elif n < n_seq:
                 raise ValueError(f"{name} has {n} states for {n_seq} sequences and no index")
-    L = _lib.lib()
+    L = _lib.rollout()
     head = (_lib.HARTS_BF16 if dtype is torch.bfloat16 else _lib.HARTS_F32, n_seq, n_rows, H, d,
             d ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr())
     tail = (_ptr(row_off), S.data_ptr(), _ptr(idx_in), n_in, S_out.data_ptr(), _ptr(idx_out), n_out, out.data_ptr())

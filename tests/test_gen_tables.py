@@ -2,17 +2,31 @@
 cover every (query row, head, segment, split) exactly once, and every entry
 point refuses what it documents before anything is enqueued."""
 import ctypes as C
+import os
+import re
 
 import numpy as np
 import pytest
 
 from oracle.gen import chain, e4m3_round, e4m3_vectors
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
 
 @pytest.fixture(scope="module")
 def L():
     from paper_2608_28158_amd import _lib
-    return _lib.lib()
+    return _lib.rollout()
+
+
+def test_library_exports_every_declared_symbol(L):
+    from paper_2608_28158_amd import _lib
+    text = open(os.path.join(ROOT, "include", "harts_rollout.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    declared = sorted(set(re.findall(r"^\s*int\s+(harts_\w+)\s*\(", text, flags=re.M)))
+    assert sorted(_lib.ROLLOUT_EXPORTS) == declared
+    for name in declared:
+        assert getattr(L, name).argtypes, name
 
 
 def tables(L, parent, n_new, cap, Hq, Hkv):
@@ -181,6 +195,7 @@ def test_attention_refuses(L):
     assert call(q=None) == E and call(o=8 * P + 8) == E and call(items=None) == E
     assert call(ws=None) == E and call(ws_bytes=8 * 4 * 66 * 4 - 1) == E
     assert call(o=7 * P) == E and call(o=7 * P + 16) == E         # o over q
+    assert call(sizes=(2 ** 62, 4, 8, 4)) == E and call(sizes=(4, 2 ** 62, 8, 4)) == E
     assert call(sizes=(-1, 4, 8, 4)) == E and call(sizes=(4, 0, 8, 4)) == E and call(sizes=(2 ** 40, 1, 1, 0)) == E
     assert call(sizes=(0, 0, 0, 0), q=None) == _lib.HARTS_OK
 
@@ -203,6 +218,7 @@ def test_steps_refuse(L):
         assert call(kda, So=16 * P, n_out=1) == E                                  # in place, two sizes
         assert call(kda, So=16 * P + 16) == E                                      # overlap
         assert call(kda, n_seq=0, q=None) == _lib.HARTS_OK
+        assert call(kda, n_in=2 ** 62) == U and call(kda, n_seq=2 ** 40, n_rows=2 ** 40) == U
     assert call(True, beta=None) == E
 
 

@@ -208,6 +208,7 @@ FORESTS = {
     "page_edges": ([-1] * 5, [63, 64, 65, 128, 129], [1, 1, 2, 1, 3]),
     "two_samples": ([-1, 0, 0], [100, 1, 33], [0, 1, 1]),
     "long_prefix": ([-1] + [0] * 9, [2500] + [1, 64, 7, 200, 31, 33, 65, 128, 96], [0] + [1] * 9),
+    "short_prefix": ([-1] + [0] * 9, [300] + [1, 64, 7, 200, 31, 33, 65, 128, 96], [0] + [1] * 9),
     "forest_any_order": ([3, 3, -1, -1, 0, 0, 1, 2], [40, 65, 500, 130, 9, 1, 70, 5], [0, 2, 1, 3, 9, 1, 4, 5]),
     "empty_segments": ([-1, 0, 1, 1, -1], [0, 70, 0, 3, 0], [0, 0, 0, 2, 0]),
     "rows_seeing_nothing": ([-1, -1, 1], [2, 0, 1], [5, 2, 3]),
