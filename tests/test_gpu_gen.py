@@ -333,6 +333,33 @@ def test_pages_that_do_not_exist_hold_no_keys():
     assert not f64(o3).any() and np.all(f64(l3) == -np.inf)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_offsets_past_32_bits(kind):
+    """Pages whose first element lies past 2^32 bytes and 2^31 elements, and one far below."""
+    from paper_2608_28158_amd.rollout import RolloutBatch, RolloutCache
+    rng = np.random.default_rng(7)
+    H, d, n_pages = 40, 128, 13500
+    assert (n_pages - 10) * H * 64 * d > 2 ** 32
+    c = RolloutCache(n_pages, 2, 3, H, d, kind=kind)
+    lens = [150, 70]
+    c.pages[0] = torch.tensor([n_pages - 1, 4, n_pages - 3], dtype=torch.int32)
+    c.pages[1, :2] = torch.tensor([n_pages - 2, 0], dtype=torch.int32)
+    c.len.copy_(torch.tensor(lens, dtype=torch.int32))
+    K, V = [], []
+    for s, n in enumerate(lens):
+        k, v = (bf16_values(rng.standard_normal((n, H, d))) for _ in range(2))
+        rows = table([(s, p) for p in range(n)])
+        c.write(rows, k.cuda(), v.cuda())
+        K.append(stands_for(k, kind))
+        V.append(stands_for(v, kind))
+        kb, vb = c.read(rows)
+        assert np.array_equal(f64(kb), K[s]) and np.array_equal(f64(vb), V[s])
+    for new in ([0, 1], [0, 70]):                            # few rows, and a tile of many
+        q = bf16_values(rng.standard_normal((sum(new), H, d)))
+        o, lse = RolloutBatch(c, [-1, 0], new, H, capacity=lens).attend(q.cuda())
+        compare(o, lse, forest_decode([-1, 0], new, K, V, f64(q), d ** -0.5), d)
+
+
 def test_runs_are_bitwise_equal():
     from paper_2608_28158_amd.rollout import RolloutBatch
     rng = np.random.default_rng(6)

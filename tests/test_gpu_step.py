@@ -123,6 +123,23 @@ def test_indexes_outside_and_repeated(kda):
 
 
 @pytest.mark.parametrize("kda", [False, True])
+def test_pools_past_32_bits(kda):
+    """States past 2^31 elements, and the variant that goes around the cache (more than 128 MiB of states)."""
+    rng = np.random.default_rng(6)
+    H, d, n, slots = 16, 128, 160, 8300
+    assert (slots - n) * H * d * d > 2 ** 31 - 2 ** 26 and n * H * d * d * 4 > 128 << 20
+    x = draw(rng, n, H, d, "bf16", kda, 1)
+    S = torch.zeros((slots, H, d, d), device="cuda")
+    first = torch.from_numpy(rng.standard_normal((2, H, d, d)).astype(np.float32)).cuda()
+    idx = torch.arange(slots - n, slots, dtype=torch.int32, device="cuda").flip(0).contiguous()
+    S[slots - 1], S[slots - n] = first[0], first[1]
+    o = call(kda, x, S=S, idx_in=idx)
+    for i, s0 in ((0, first[0]), (n - 1, first[1]), (n // 2, torch.zeros_like(first[0]))):
+        y = {m: (v[i:i + 1] if m != "S" else s0.cpu()[None]) for m, v in x.items()}
+        check(kda, y, [0, 1], [0], o[i:i + 1], S[int(idx[i])][None], [0], d ** -0.5, "bf16")
+
+
+@pytest.mark.parametrize("kda", [False, True])
 def test_decays_of_zero_and_minus_infinity(kda):
     rng = np.random.default_rng(4)
     x = draw(rng, 2, 1, 64, "f32", kda, 2)
