@@ -230,14 +230,14 @@ def lib():
     return L
 
 
-_rollout = None
+_rollout_lib = None
 
 
 def rollout():
     """The library with the generation calls (include/harts_rollout.h) declared."""
-    global _rollout
-    if _rollout is not None:
-        return _rollout
+    global _rollout_lib
+    if _rollout_lib is not None:
+        return _rollout_lib
     L = lib()
     vp, sz, i32, i64, f32 = C.c_void_p, C.c_size_t, C.c_int32, C.c_int64, C.c_float
     for name, args in (
@@ -251,8 +251,28 @@ def rollout():
             ("harts_kda_step", [i32, i64, i64, i32, i32, f32] + [vp] * 8 + [i64, vp, vp, i64, vp, vp])):
         fn = getattr(L, name)
         fn.restype, fn.argtypes = C.c_int, args
-    _rollout = L
+    _rollout_lib = L
     return L
+
+
+_binding = None
+
+
+def rollout_binding():
+    """The torch binding of the generation calls (_rollout.so, built beside the
+    library), bound to the loaded library's functions."""
+    global _binding
+    if _binding is None:
+        L = rollout()
+        try:
+            from . import _rollout as ext
+        except ImportError as e:
+            raise RuntimeError("_rollout.so not found; build it with "
+                               "`python -c 'import __graft_entry__ as g; g.build()'`") from e
+        ext.bind(*(C.cast(getattr(L, name), C.c_void_p).value for name in (
+            "harts_cache_write", "harts_cache_read", "harts_gen_attn", "harts_la_step", "harts_kda_step")), check)
+        _binding = ext
+    return _binding
 
 
 def profile_begin():

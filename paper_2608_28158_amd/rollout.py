@@ -2,7 +2,8 @@
 rows over its segments, and the recurrent steps of the linear layers.  Argument
 marshalling around harts_cache_*, harts_gen_* and harts_*_step of libharts.so;
 every step runs in the library's kernels, on the current stream of the
-tensors' device.
+tensors' device.  The calls check their arguments and launch in a compiled
+binding (csrc/rollout_ext.cpp): a token is many small ones.
 
 A forest here is what the batch in flight looks like: a segment is a run of
 rows that its descendants share (a prompt, a branch, the tail of one rollout),
@@ -40,41 +41,10 @@ def _device(device):
     return d if d.index is not None else torch.device("cuda", torch.cuda.current_device())
 
 
-# The current stream's handle and device without the objects and the lazy
-# initialisation around them (0.2 us instead of 1.4, of a small call's 7), where
-# torch offers that.
+# The current stream's handle without a Stream object around it (0.1 us instead
+# of 1.2, of a small call's 5), where torch offers that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
-_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-
-
-def _call(index, what, fn, *args):
-    """fn(*args, stream) on the tensors' device: the library launches on the current one."""
-    if _current() == index:
-        code = fn(*args, _raw_stream(index))
-    else:
-        with torch.cuda.device(index):
-            code = fn(*args, _raw_stream(index))
-    if code:
-        _lib.check(code, what)
-
-
-def _check(shape, dtype, device, names, *tensors):
-    """Contiguous tensors of one shape, type and device, none of them recording a gradient."""
-    for t in tensors:
-        if (t.dtype is not dtype or t.shape != shape or not t.is_contiguous() or t.device != device or
-                t.requires_grad):
-            break
-    else:
-        return
-    for name, t in zip(names.split(), tensors):
-        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}"
-                             f"{'' if t.is_contiguous() else ' with strides ' + str(t.stride())}")
-        if t.device != device:
-            raise ValueError(f"{name} is on {t.device}, expected {device}")
-        if t.requires_grad and torch.is_grad_enabled():
-            raise RuntimeError(f"{name} requires a gradient; generation is not differentiable")
 
 
 class RolloutCache:
@@ -90,7 +60,7 @@ class RolloutCache:
             raise ValueError("kind must be 'bf16' or 'e4m3'")
         if min(n_pages, n_seg, pitch, heads, layers) < 1 or d not in (64, 128):
             raise ValueError("need at least one page, segment, column, head and layer, and d in {64, 128}")
-        self.L, self.device = _lib.rollout(), _device(device)
+        self.L, self._ext, self.device = _lib.rollout(), _lib.rollout_binding(), _device(device)
         self.n_pages, self.n_seg, self.pitch, self.heads, self.d = n_pages, n_seg, pitch, heads, d
         self.kind, self.layers = kind, layers
         dt = torch.bfloat16 if kind == "bf16" else torch.float8_e4m3fn
@@ -109,8 +79,9 @@ class RolloutCache:
         ptr = lambda t, i: None if t is None else t[i].data_ptr()
         fixed = (self.pages.data_ptr(), self.len.data_ptr(), n_pages, n_seg, pitch, heads, d, code)
         # (the library's view of each layer: the tensors above are written, never replaced)
-        self._desc = [C.byref(_lib.Cache(*(ptr(t, i) for t in (self.k, self.v, self.k_exp, self.v_exp)), *fixed))
-                      for i in range(layers)]
+        self._layers = [_lib.Cache(*(ptr(t, i) for t in (self.k, self.v, self.k_exp, self.v_exp)), *fixed)
+                        for i in range(layers)]
+        self._desc = [C.addressof(c) for c in self._layers]
 
     # -- pages (host bookkeeping) --------------------------------------------
     @property
@@ -155,22 +126,14 @@ class RolloutCache:
         """Rows k, v [n, heads, d] (bf16) into the cache at ``rows`` [n, 2]
         (int32 segment and position, negative from the segment's end).  A row
         may be named once; entries that name no existing row are skipped."""
-        n = rows.shape[0]
-        _check((n, 2), torch.int32, self.device, "rows", rows)
-        _check((n, self.heads, self.d), torch.bfloat16, self.device, "k v", k, v)
-        _call(self.device.index, "harts_cache_write", self.L.harts_cache_write, self.desc(layer), rows.data_ptr(), n,
-              k.data_ptr(), v.data_ptr())
+        index = self.device.index
+        self._ext.cache_write(self.desc(layer), index, _raw_stream(index), rows, k, v)
 
     def read(self, rows, layer: int = 0):
         """(k, v) [n, heads, d] bf16: what the rows stand for, zeros where an
         entry names no existing row."""
-        n = rows.shape[0]
-        _check((n, 2), torch.int32, self.device, "rows", rows)
-        k = torch.empty((n, self.heads, self.d), dtype=torch.bfloat16, device=self.device)
-        v = torch.empty_like(k)
-        _call(self.device.index, "harts_cache_read", self.L.harts_cache_read, self.desc(layer), rows.data_ptr(), n,
-              k.data_ptr(), v.data_ptr())
-        return k, v
+        index = self.device.index
+        return self._ext.cache_read(self.desc(layer), index, _raw_stream(index), rows)
 
 
 class RolloutBatch:
@@ -195,22 +158,23 @@ class RolloutBatch:
         self.sizes = _lib.GenSizes()
         _lib.check(self.L.harts_gen_layout(*host, C.byref(self.sizes)), "harts_gen_layout")
         self.n_rows = int(self.sizes.n_rows)
-        rows, order = np.zeros((self.n_rows, 2), np.int32), np.zeros(self.n_rows, np.int32)
-        items, off = np.zeros((self.sizes.n_items, 12), np.int32), np.zeros(self.n_rows + 1, np.int32)
+        # one upload: rows, order, items, part offsets and new rows, each from a multiple of 16 bytes
+        shapes = ((self.n_rows, 2), (self.n_rows,), (self.sizes.n_items, 12), (self.n_rows + 1,), (cache.n_seg,))
+        at = np.cumsum([0] + [-(-int(np.prod(s)) // 4) * 4 for s in shapes])
+        host_tab = np.zeros(int(at[-1]), np.int32)
+        part = lambda t: [t[i:i + int(np.prod(s))].reshape(s) for i, s in zip(at, shapes)]
+        rows, order, items, off, n_new = part(host_tab)
+        n_new[:] = new
         _lib.check(self.L.harts_gen_tables(*host, rows.ctypes.data, order.ctypes.data, items.ctypes.data,
                                            off.ctypes.data), "harts_gen_tables")
-        dev = lambda a: torch.from_numpy(a).to(cache.device)
-        self.rows, self._order, self._items, self._off, self.n_new = dev(rows), dev(order), dev(items), dev(off), dev(new)
+        self._tab = torch.from_numpy(host_tab).to(cache.device)
+        self.rows, order, items, off, self.n_new = part(self._tab)
         size = C.c_size_t()
         _lib.check(self.L.harts_gen_workspace_size(C.byref(self.sizes), self.q_heads, cache.d, C.byref(size)),
                    "harts_gen_workspace_size")
         self.ws_bytes = size.value
-        # shapes to allocate by: one element each, expanded (0.5 us less a call than a shape and a type)
-        like = lambda shape, dtype: torch.empty(1, dtype=dtype, device=cache.device).expand(shape)
-        self._lse, self._ws = like((self.n_rows, self.q_heads), torch.float32), like((self.ws_bytes,), torch.uint8)
-        self._shape = torch.Size((self.n_rows, self.q_heads, cache.d))
-        self._tables = (C.byref(self.sizes), self._items.data_ptr(), self._order.data_ptr(), self._off.data_ptr(),
-                        self.q_heads)
+        self._call = (C.addressof(self.sizes), items.data_ptr(), order.data_ptr(), off.data_ptr(), self.q_heads,
+                      self.ws_bytes, cache.device.index)
 
     def advance(self):
         """The segments' lengths grow by their new rows."""
@@ -224,75 +188,7 @@ class RolloutBatch:
         """(o [n_rows, q_heads, d] bf16, lse [n_rows, q_heads] float32) of the
         new rows' queries; scale defaults to d ** -0.5."""
         c = self.cache
-        _check(self._shape, torch.bfloat16, c.device, "q", q)
-        if out is None:
-            out = torch.empty_like(q)
-        else:
-            _check(self._shape, torch.bfloat16, c.device, "out", out)
-        # (from the allocator at every call: calls on other streams, or captured into other graphs, share none)
-        lse = torch.empty_like(self._lse)
-        ws = torch.empty_like(self._ws) if self.ws_bytes else None
-        _call(c.device.index, "harts_gen_attn", self.L.harts_gen_attn, c.desc(layer), *self._tables,
-              c.d ** -0.5 if scale is None else scale, q.data_ptr(), out.data_ptr(), lse.data_ptr(), _ptr(ws),
-              self.ws_bytes)
-        return out, lse
-
-
-def _ptr(t):
-    return None if t is None else t.data_ptr()
-
-
-def _step(kda, q, k, v, g, beta, S, S_out, idx_in, idx_out, row_off, scale, out):
-    shape, dtype, dev = q.shape, q.dtype, q.device
-    if len(shape) != 3 or (dtype is not torch.bfloat16 and dtype is not torch.float32):
-        raise ValueError("q must be float32 or bfloat16 [rows, H, d]")
-    if dev.type != "cuda":
-        raise RuntimeError("generation runs on the GPU only")
-    n_rows, H, d = shape
-    if out is None:
-        _check(shape, dtype, dev, "q k v", q, k, v)
-        out = torch.empty_like(q)
-    else:
-        _check(shape, dtype, dev, "q k v out", q, k, v, out)
-    _check(shape if kda else (n_rows, H), torch.float32, dev, "g", g)
-    if kda:
-        _check((n_rows, H), torch.float32, dev, "beta", beta)
-    n_seq = n_rows
-    if row_off is not None:
-        n_seq = row_off.numel() - 1
-        if n_seq < 0:
-            raise ValueError("row_off has one entry more than there are sequences")
-        _check((n_seq + 1,), torch.int32, dev, "row_off", row_off)
-    if S_out is None:
-        if idx_out is not None:
-            raise ValueError("an update in place leaves every state where it was: idx_out has to be None")
-        S_out, idx_out = S, idx_in
-    elif S_out is S and idx_out is not idx_in:
-        raise ValueError("an update in place leaves every state where it was: S_out and idx_out have to be None")
-    n_in, n_out = len(S), len(S_out)
-    if S_out is S or n_out != n_in:
-        _check((n_in, H, d, d), torch.float32, dev, "S", S)
-        if S_out is not S:
-            _check((n_out, H, d, d), torch.float32, dev, "S_out", S_out)
-    else:
-        _check((n_in, H, d, d), torch.float32, dev, "S S_out", S, S_out)
-    if idx_in is not None and idx_out is not None:
-        _check((n_seq,), torch.int32, dev, "idx_in idx_out", idx_in, idx_out)
-    else:
-        for idx, n, name in ((idx_in, n_in, "S"), (idx_out, n_out, "S_out")):
-            if idx is not None:
-                _check((n_seq,), torch.int32, dev, "index", idx)
-            elif n < n_seq:
-                raise ValueError(f"{name} has {n} states for {n_seq} sequences and no index")
-    L = _lib.rollout()
-    head = (_lib.HARTS_BF16 if dtype is torch.bfloat16 else _lib.HARTS_F32, n_seq, n_rows, H, d,
-            d ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr())
-    tail = (_ptr(row_off), S.data_ptr(), _ptr(idx_in), n_in, S_out.data_ptr(), _ptr(idx_out), n_out, out.data_ptr())
-    if kda:
-        _call(dev.index, "harts_kda_step", L.harts_kda_step, *head, beta.data_ptr(), *tail)
-    else:
-        _call(dev.index, "harts_la_step", L.harts_la_step, *head, *tail)
-    return out
+        return c._ext.attend(c.desc(layer), *self._call, _raw_stream(c.device.index), q, scale, out)
 
 
 def la_step(q, k, v, g, S, S_out=None, idx_in=None, idx_out=None, row_off=None, scale=None, out=None):
@@ -301,9 +197,11 @@ def la_step(q, k, v, g, S, S_out=None, idx_in=None, idx_out=None, row_off=None, 
     [row_off[i], row_off[i + 1]) one after the other.  States start from
     S[idx_in[i]] and end in S_out[idx_out[i]] (no index: i; no S_out: in
     place).  Several sequences may start from one state: a fork.  Returns o."""
-    return _step(False, q, k, v, g, None, S, S_out, idx_in, idx_out, row_off, scale, out)
+    return _lib.rollout_binding().step(False, q, k, v, g, None, S, S_out, idx_in, idx_out, row_off, scale, out,
+                                       _raw_stream)
 
 
 def kda_step(q, k, v, g, beta, S, S_out=None, idx_in=None, idx_out=None, row_off=None, scale=None, out=None):
     """The same for KDA: g [rows, H, d], beta [rows, H]."""
-    return _step(True, q, k, v, g, beta, S, S_out, idx_in, idx_out, row_off, scale, out)
+    return _lib.rollout_binding().step(True, q, k, v, g, beta, S, S_out, idx_in, idx_out, row_off, scale, out,
+                                       _raw_stream)
