@@ -83,7 +83,8 @@ int harts_cache_read(const harts_cache* cache, const int32_t* rows, int64_t n, v
  *   items    [n_items][12] out: work items (segment, first place in order,
  *            first stacked row, stacked rows, split, splits, new rows of the
  *            segment, part of a row's first part, 16-row tiles of a wave,
- *            waves along rows, 2 unused); a stacked row is one of the Hq/Hkv
+ *            waves along rows, multiplier and shift that divide by splits); a
+ *            stacked row is one of the Hq/Hkv
  *            query heads of one query row.
  *   part_off [n_rows + 1] out: partial results of every row (in q's order).
  *   Errors: HARTS_EINVAL (NULL, sizes, a parent out of range or a cycle),

@@ -46,6 +46,7 @@
 #include <string>
 #include <type_traits>
 
+#include "fast_div.hpp"
 #include "gen.hpp"
 #include "harts_rollout.h"
 #include "la_common.hpp"
@@ -74,6 +75,7 @@ struct CacheView {
   uint8_t *ke, *ve;
   const int32_t *pages, *len;
   int32_t n_pages, n_seg, pitch, H;
+  FastDiv by_heads;
 };
 
 // Index of (row, head 0) as page * H * 64 + slot of a row table's entry, or -1
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(GEN_THR) void k_cache_write(CacheView c, const int3
   const int64_t rh = i / P;
   const int piece = static_cast<int>(i % P);
   if (rh >= n * c.H) return;
-  const int64_t r = rh / c.H;
+  const int64_t r = c.by_heads.div(static_cast<u32>(rh));   // (n H < 2^31)
   const int h = static_cast<int>(rh - r * c.H);
   u32x4 a, b;
   if constexpr (!E4M3 && NT) {
@@ -184,7 +186,7 @@ __global__ __launch_bounds__(GEN_THR) void k_cache_read(CacheView c, const int32
   const int64_t rh = i / P;
   const int piece = static_cast<int>(i % P);
   if (rh >= n * c.H) return;
-  const int64_t r = rh / c.H;
+  const int64_t r = c.by_heads.div(static_cast<u32>(rh));   // (n H < 2^31)
   const int h = static_cast<int>(rh - r * c.H);
   const int64_t at = cache_row(c, rows[2 * r], rows[2 * r + 1]);
   u32x4 a{0, 0, 0, 0}, b{0, 0, 0, 0};
@@ -342,6 +344,7 @@ struct GenArgs {
   CacheView c;
   const int32_t *items, *order, *part_off;
   int32_t Hq;
+  FastDiv by_group, by_Hq;     // query heads of a key head; all
   float scale;                 // |scale| * log2(e)
   u32 sign;                    // 0x80008000 where the scale is negative: q's signs change instead, so
                                // that the largest product is the largest score
@@ -352,6 +355,11 @@ struct GenArgs {
 
 __device__ inline bf16x8 q_frag(const GenArgs& A, const bf16* p) {
   return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p) ^ A.sign);
+}
+
+// Place below its segment of a stacked row.
+__device__ inline int place_of(const GenArgs& A, int stacked) {
+  return static_cast<int>(A.by_group.div(static_cast<u32>(stacked)));
 }
 
 // What an item's rows see: rows of the segment that exist (n), all that were
@@ -375,7 +383,8 @@ struct Reach {
 template <int T>
 __device__ inline void split_steps(Scalars it, int32_t hi, int32_t& from, int32_t& to) {
   const int32_t steps = (hi + T - 1) / T, n = it[GI_SPLITS];
-  const int32_t per = (steps + n - 1) / n;
+  const FastDiv by(n, static_cast<u32>(it[GI_MUL]), static_cast<u32>(it[GI_SHIFT]));
+  const int32_t per = static_cast<int32_t>(by.div(static_cast<u32>(steps + n - 1)));
   from = static_cast<int32_t>(min(static_cast<int64_t>(it[GI_SPLIT]) * per, static_cast<int64_t>(steps)));
   to = min(from + per, steps);
 }
@@ -446,7 +455,7 @@ __device__ inline void add_odd(const CacheView& c, Scalars table, int hk, int32_
     }
 }
 
-constexpr int GEN_JOIN = 35;   // floats a lane leaves in LDS for a join at D = 128
+constexpr int GEN_JOIN = 9;    // 16-byte pieces that a lane leaves in LDS for a join at D = 128
 
 // Few rows: 16 of them a wave; one, two or four (GI_WAVES) waves along the rows,
 // the others share the keys.
@@ -458,19 +467,19 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
   // D = 128, 64 8-bit keys spill: 64 rows of 2,000 keys, 8 heads 111 us against 63)
   constexpr int NK = E4M3 && D == 64 ? 2 : 1, T = 32 * NK;
   constexpr int DT = D / 16;                        // 16-column tiles
-  static_assert(3 + 4 * DT <= GEN_JOIN, "room for a join");
+  static_assert(DT + 1 <= GEN_JOIN, "room for a join");
   const CacheView& c = A.c;
-  const int rw = it[GI_WAVES], kws = 4 / rw;
-  const int rt = wave % rw, kw = wave / rw;
-  const int seg = it[GI_SEG], group = A.Hq / c.H;
+  const int rw = it[GI_WAVES], sh = rw >> 1, kws = 4 >> sh;   // (1, 2 or 4)
+  const int rt = wave & (rw - 1), kw = wave >> sh;
+  const int seg = it[GI_SEG], group = static_cast<int>(A.by_group.d);
   const int g = lane >> 4, i = lane & 15;
   const Reach reach(c, seg, it[GI_NEW]);
   const int32_t n = reach.n;
 
   const int local = 16 * rt + i;
   const bool live = local < it[GI_N];
-  const int stacked = it[GI_ROW] + (live ? local : 0), place = stacked / group;
-  const int32_t row = A.order[it[GI_FIRST] + place], head = hk * group + stacked % group;
+  const int stacked = it[GI_ROW] + (live ? local : 0), place = place_of(A, stacked);
+  const int32_t row = A.order[it[GI_FIRST] + place], head = hk * group + stacked - place * group;
   const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
   int32_t lim = reach.of(place);
   bf16x8 qf[D / 32];
@@ -481,8 +490,8 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
   // it, and what a row sees with its place (own rows one more each, then the
   // descendants', which see all)
   const int first = 16 * rt, last = min(first + 16, it[GI_N]) - 1;
-  const int32_t lo = last < first ? n : reach.of((it[GI_ROW] + first) / group);
-  const int32_t hi = last < first ? 0 : reach.of((it[GI_ROW] + last) / group);
+  const int32_t lo = last < first ? n : reach.of(place_of(A, it[GI_ROW] + first));
+  const int32_t hi = last < first ? 0 : reach.of(place_of(A, it[GI_ROW] + last));
   if (!live) lim = n;                               // padding rows take part and are dropped
 
   int32_t from, end;
@@ -576,30 +585,27 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
   }
   st.sum = over_groups_sum(st.sum);
 
-  // join the waves that shared the keys, half of them into the other half
+  // join the waves that shared the keys, half of them into the other half: 16
+  // bytes a lane at a time, as short a code as a once-run one should be
+  typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
   for (int step = kws / 2; step >= 1; step /= 2) {
     if (kw >= step && kw < 2 * step) {
-      float* p = lds + ((kw - step) * rw + rt) * (64 * GEN_JOIN) + lane;
-      p[0] = st.ref;
-      p[64] = st.sum;
-      p[128] = odds ? 1.f : 0.f;
+      lds_f32x4* p = (lds_f32x4*)lds + ((kw - step) * rw + rt) * (64 * GEN_JOIN) + lane;
 #pragma unroll
-      for (int j = 0; j < DT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[64 * (3 + 4 * j + e)] = st.acc[j][e];
+      for (int j = 0; j < DT; ++j) p[64 * j] = st.acc[j];
+      p[64 * DT] = f32x4{st.ref, st.sum, odds ? 1.f : 0.f, 0.f};
     }
     __syncthreads();
     if (kw < step) {
-      const float* p = lds + (kw * rw + rt) * (64 * GEN_JOIN) + lane;
-      const float r1 = p[0], s1 = p[64], to = fmaxf(st.ref, r1), r = to == -INFINITY ? 0.f : to;
-      const float f0 = __builtin_amdgcn_exp2f(st.ref - r), f1 = __builtin_amdgcn_exp2f(r1 - r);
+      const lds_f32x4* p = (const lds_f32x4*)lds + (kw * rw + rt) * (64 * GEN_JOIN) + lane;
+      const f32x4 head = p[64 * DT];
+      const float to = fmaxf(st.ref, head[0]), r = to == -INFINITY ? 0.f : to;
+      const float f0 = __builtin_amdgcn_exp2f(st.ref - r), f1 = __builtin_amdgcn_exp2f(head[0] - r);
       st.ref = to;
-      st.sum = st.sum * f0 + s1 * f1;
-      odds |= p[128] != 0.f;
+      st.sum = st.sum * f0 + head[1] * f1;
+      odds |= head[2] != 0.f;
 #pragma unroll
-      for (int j = 0; j < DT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) st.acc[j][e] = st.acc[j][e] * f0 + p[64 * (3 + 4 * j + e)] * f1;
+      for (int j = 0; j < DT; ++j) st.acc[j] = st.acc[j] * f0 + p[64 * j] * f1;
     }
     if (step > 1) __syncthreads();
   }
@@ -746,13 +752,13 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
   constexpr int T = gen_step<D>(), NS = D / 32, DT = D / 16, TILE = T * D, ROWB = E4M3 ? D : 2 * D;
   typedef GenTile<D> L;
   const CacheView& c = A.c;
-  const int seg = it[GI_SEG], group = A.Hq / c.H, m = it[GI_N];
+  const int seg = it[GI_SEG], group = static_cast<int>(A.by_group.d), m = it[GI_N];
   const int g = lane >> 4, i = lane & 15;
   const Reach reach(c, seg, it[GI_NEW]);
   const int32_t n = reach.n;
   // (as in gen_few; lo of the tile, so that all waves go over to the masked steps together)
-  const int32_t lo = reach.of(it[GI_ROW] / group), most = reach.of((it[GI_ROW] + m - 1) / group);
-  const int32_t hi = 32 * wave < m ? reach.of((it[GI_ROW] + min(32 * wave + 32, m) - 1) / group) : 0;
+  const int32_t lo = reach.of(place_of(A, it[GI_ROW])), most = reach.of(place_of(A, it[GI_ROW] + m - 1));
+  const int32_t hi = 32 * wave < m ? reach.of(place_of(A, it[GI_ROW] + min(32 * wave + 32, m) - 1)) : 0;
   int32_t from, end;
   split_steps<T>(it, most, from, end);
 
@@ -791,8 +797,8 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
   bf16x8 qf[2][NS];
 #pragma unroll
   for (int a = 0; a < 2; ++a) {
-    const int r = stacked_of(a);
-    const int64_t row = A.order[it[GI_FIRST] + r / group], head = hk * group + r % group;
+    const int r = stacked_of(a), place = place_of(A, r);
+    const int64_t row = A.order[it[GI_FIRST] + place], head = hk * group + r - place * group;
     const bf16* qp = A.q + (row * A.Hq + head) * D + 8 * g;
 #pragma unroll
     for (int s = 0; s < NS; ++s) qf[a][s] = q_frag(A, qp + 32 * s);
@@ -830,7 +836,8 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
         s[1][j] = mfma32(kf, qf[1][d], s[1][j]);
       }
     __builtin_amdgcn_s_setprio(0);
-    const int32_t lim[2] = {edge ? reach.of(stacked_of(0) / group) : 0, edge ? reach.of(stacked_of(1) / group) : 0};
+    const int32_t lim[2] = {edge ? reach.of(place_of(A, stacked_of(0))) : 0,
+                            edge ? reach.of(place_of(A, stacked_of(1))) : 0};
     float top[2];
     bool up = false;
 #pragma unroll
@@ -898,8 +905,9 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
   for (int a = 0; a < 2; ++a) {
     st[a].sum = over_groups_sum(st[a].sum);
     if (32 * wave + 16 * a + i >= m) continue;
-    const int r = stacked_of(a), row = A.order[it[GI_FIRST] + r / group], head = hk * group + r % group;
-    const int32_t lim = reach.of(r / group);
+    const int r = stacked_of(a), place = place_of(A, r);
+    const int32_t row = A.order[it[GI_FIRST] + place], head = hk * group + r - place * group;
+    const int32_t lim = reach.of(place);
     const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
     if (parts == 1) {
       const int64_t rh = static_cast<int64_t>(row) * A.Hq + head;
@@ -930,9 +938,9 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
 template <int D, bool E4M3>
 __global__ __launch_bounds__(GEN_THR, 3) void k_gen_attn(GenArgs A) {
   constexpr int TILE = gen_step<D>() * D * 2;      // bytes
-  static_assert(4 * TILE >= 2 * 64 * GEN_JOIN * 4, "a join fits");
+  static_assert(4 * TILE >= 2 * 64 * GEN_JOIN * 16, "a join fits");
   __shared__ __align__(16) char lds[E4M3 ? 5 * TILE : 4 * TILE];
-  const int item = blockIdx.x / A.c.H, hk = blockIdx.x % A.c.H;
+  const int item = static_cast<int>(A.c.by_heads.div(blockIdx.x)), hk = blockIdx.x - item * A.c.H;
   const Scalars it = scalars(A.items) + static_cast<int64_t>(item) * GI_WORDS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (it[GI_TILES] == 1) gen_few<D, E4M3>(A, it, hk, wave, lane, reinterpret_cast<float*>(lds));
@@ -952,8 +960,8 @@ __global__ __launch_bounds__(GEN_THR) void k_gen_join(GenArgs A, int64_t n) {
   const int64_t rh = static_cast<int64_t>(blockIdx.x) * ENTRIES + grp / SUBS;
   int32_t p0 = 0, parts = 0, head = 0;
   if (rh < n) {
-    const int32_t row = static_cast<int32_t>(rh / A.Hq);
-    head = static_cast<int32_t>(rh % A.Hq);
+    const int32_t row = static_cast<int32_t>(A.by_Hq.div(static_cast<u32>(rh)));
+    head = static_cast<int32_t>(rh - static_cast<int64_t>(row) * A.Hq);
     p0 = A.part_off[row];
     parts = A.part_off[row + 1] - p0;
   }
@@ -1044,7 +1052,7 @@ int check_cache(const harts_cache* c, const char* where) {
 
 CacheView view_of(const harts_cache* c) {
   return {static_cast<char*>(c->k), static_cast<char*>(c->v), c->k_exp, c->v_exp, c->pages, c->len,
-          c->n_pages, c->n_seg, c->pitch, c->H};
+          c->n_pages, c->n_seg, c->pitch, c->H, FastDiv(static_cast<u32>(c->H))};
 }
 
 // f(head size, whether 8-bit) of a cache, as constants
@@ -1076,7 +1084,7 @@ int check_rows(const harts_cache* c, const int32_t* rows, int64_t n, const void*
     set_error(std::string(where) + ": NULL or misaligned pointer");
     return HARTS_EINVAL;
   }
-  if (n > INT32_MAX || piece_blocks(n, c) == 0) {
+  if (n > INT32_MAX / c->H || piece_blocks(n, c) == 0) {
     set_error(std::string(where) + ": too many rows for one call");
     return HARTS_EUNSUPPORTED;
   }
@@ -1161,6 +1169,8 @@ extern "C" int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* s
   A.order = order;
   A.part_off = part_off;
   A.Hq = Hq;
+  A.by_group = FastDiv(static_cast<u32>(Hq / cache->H));
+  A.by_Hq = FastDiv(static_cast<u32>(Hq));
   A.scale = fabsf(scale) * GEN_LOG2E;
   A.sign = scale < 0.f ? 0x80008000u : 0u;
   A.q = static_cast<const bf16*>(q);

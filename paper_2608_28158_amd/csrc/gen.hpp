@@ -21,6 +21,8 @@ enum GenItem : int {
   GI_PART = 7,    // a row's first part in the segment
   GI_TILES = 8,   // 16-row tiles of a wave: 1 or 2
   GI_WAVES = 9,   // waves along the rows: 1, 2 or 4; where fewer than 4, the others share the keys
+  GI_MUL = 10,    // multiplier and
+  GI_SHIFT = 11,  // shift that divide by GI_SPLITS (fast_div.hpp)
   GI_WORDS = 12
 };
 

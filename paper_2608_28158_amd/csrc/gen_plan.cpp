@@ -13,6 +13,7 @@
 #include <string>
 #include <vector>
 
+#include "fast_div.hpp"
 #include "gen.hpp"
 #include "harts_rollout.h"
 #include "plan.hpp"
@@ -226,7 +227,9 @@ extern "C" int harts_gen_tables(int32_t n_seg, const int32_t* parent, const int3
       w[GI_PART] = P.base[it.seg];
       w[GI_TILES] = f.tiles;
       w[GI_WAVES] = f.waves;
-      w[GI_WORDS - 2] = w[GI_WORDS - 1] = 0;
+      const FastDiv by(static_cast<uint32_t>(P.splits[it.seg]));
+      w[GI_MUL] = static_cast<int32_t>(by.m);
+      w[GI_SHIFT] = static_cast<int32_t>(by.s);
       w += GI_WORDS;
     }
   } catch (const std::bad_alloc&) {

@@ -21,6 +21,7 @@
 #include <string>
 #include <type_traits>
 
+#include "fast_div.hpp"
 #include "harts_rollout.h"
 #include "la_common.hpp"
 #include "plan.hpp"
@@ -35,6 +36,7 @@ struct StepArgs {
   int64_t n_seq, n_rows;
   int32_t H;
   float scale;
+  FastDiv by_heads;
   const void *q, *k, *v;
   const float *g, *beta;
   const int32_t* row_off;
@@ -95,10 +97,9 @@ template <typename T, int D, bool KDA, bool NT>
 __global__ __launch_bounds__(ST_THR) void k_step(StepArgs A) {
   constexpr int NR = D / 8, SLABS = D / ST_COLS;
   const int lane = threadIdx.x & 63;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * (ST_THR / 64) +
-                       __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t head = unit / SLABS;               // sequence * H + head
-  const int64_t seq = head / A.H;
+  const uint32_t unit = blockIdx.x * (ST_THR / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t head = unit / SLABS;              // sequence * H + head
+  const int64_t seq = A.by_heads.div(head);
   if (seq >= A.n_seq) return;
   const int h = static_cast<int>(head - seq * A.H);
   const int r = lane >> 3, col = static_cast<int>(unit % SLABS) * ST_COLS + 4 * (lane & 7);
@@ -234,12 +235,14 @@ int step(const char* where, int32_t dtype, int32_t d, const StepArgs& A, void* s
     if ((a < b ? b - a : a - b) < span) return fail(HARTS_EINVAL, "o overlaps an input");
   }
   const int64_t blocks = (A.n_seq * A.H * (d / ST_COLS) + ST_THR / 64 - 1) / (ST_THR / 64);
-  if (blocks > INT32_MAX) return fail(HARTS_EUNSUPPORTED, "too many sequences for one call");
+  if (A.n_seq * A.H * (d / ST_COLS) > INT32_MAX - ST_THR) return fail(HARTS_EUNSUPPORTED, "too many sequences for one call");
   // States past what the last-level cache holds are not kept in it (512 sequences,
   // 16 heads of 128, two pools of 512 MiB: 214 us, 198 so; 64 sequences 23, 25 so).
   const bool nt = A.n_seq * state > (size_t{128} << 20);
+  StepArgs B = A;
+  B.by_heads = FastDiv(static_cast<uint32_t>(A.H));
   const auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(ST_THR), 0, static_cast<hipStream_t>(stream), A);
+    hipLaunchKernelGGL(kernel, dim3(static_cast<uint32_t>(blocks)), dim3(ST_THR), 0, static_cast<hipStream_t>(stream), B);
   };
   const auto pick = [&](auto type, auto dim) {
     typedef decltype(type) T;
@@ -265,7 +268,7 @@ extern "C" int harts_la_step(int32_t dtype, int64_t n_seq, int64_t n_rows, int32
                              const float* S_in, const int32_t* idx_in, int64_t n_in, float* S_out,
                              const int32_t* idx_out, int64_t n_out, void* o, void* stream) {
   return step<false>("harts_la_step", dtype, d,
-                     {n_seq, n_rows, H, scale, q, k, v, g, nullptr, row_off, S_in, idx_in, n_in, S_out, idx_out, n_out, o},
+                     {n_seq, n_rows, H, scale, {}, q, k, v, g, nullptr, row_off, S_in, idx_in, n_in, S_out, idx_out, n_out, o},
                      stream);
 }
 
@@ -274,6 +277,6 @@ extern "C" int harts_kda_step(int32_t dtype, int64_t n_seq, int64_t n_rows, int3
                               const int32_t* row_off, const float* S_in, const int32_t* idx_in, int64_t n_in,
                               float* S_out, const int32_t* idx_out, int64_t n_out, void* o, void* stream) {
   return step<true>("harts_kda_step", dtype, d,
-                    {n_seq, n_rows, H, scale, q, k, v, g, beta, row_off, S_in, idx_in, n_in, S_out, idx_out, n_out, o},
+                    {n_seq, n_rows, H, scale, {}, q, k, v, g, beta, row_off, S_in, idx_in, n_in, S_out, idx_out, n_out, o},
                     stream);
 }
