@@ -656,19 +656,28 @@ struct GenTile {
     const int hi = (r >> 3) & 1;
     return D == 128 ? (((r & 7) ^ (hi << 2)) << 1) | hi : ((r & 6) ^ (hi << 2)) | hi;
   }
-  // lane (g, i): key k0 + i (k0 a multiple of 16), columns 32 s + 8 g .. + 7
-  __device__ static inline bf16x8 rows(const bf16* t, int k0, int s, int lane) {
-    typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+  // Reads by LDS addresses.  A tile starts at a multiple of its row's bytes, so a
+  // column's piece goes into the address by exclusive or, and two constants of
+  // the lane (and one or two of the step) serve all fragments.
+  __device__ static inline u32 rows_lane(int lane) {
     const int i = lane & 15, g = lane >> 4;
-    return *(const lds_bf16x8*)(t + (k0 + i) * D + (((4 * s + g) ^ swz(i)) << 3));
+    return 2 * D * i + ((g ^ swz(i)) << 4);
   }
-  // lane (g, i): column c0 + i, keys k0 + frag_key(g, 0 .. 7)
-  __device__ static inline bf16x8 columns(const bf16* t, int k0, int c0, int lane) {
-    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+  __device__ static inline u32 columns_lane(int lane) {
     const int r = (lane >> 4) * 4 + ((lane & 15) >> 2), c = lane & 3;
-    const bf16* p = t + (k0 + r) * D + ((((c0 >> 3) + (c >> 1)) ^ swz(r)) << 3) + 4 * (c & 1);
+    return 2 * D * r + (((c >> 1) ^ swz(r)) << 4) + 8 * (c & 1);
+  }
+  // lane (g, i): key 16 j + i, columns 32 s + 8 g .. + 7
+  __device__ static inline bf16x8 rows(u32 at, int j, int s) {
+    typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+    return *(const lds_bf16x8*)((at ^ (s << 6)) + j * 32 * D);
+  }
+  // lane (g, i): column 16 j + i, keys 32 h + frag_key(g, 0 .. 7)
+  __device__ static inline bf16x8 columns(u32 at, int h, int j) {
+    typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+    const u32 p = (at ^ (j << 5)) + h * 64 * D;
     const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
-    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 16 * D));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 32 * D));
     return Frag<bf16>::join(__builtin_bit_cast(bf16x4, lo), __builtin_bit_cast(bf16x4, hi));
   }
 };
@@ -807,6 +816,7 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
   st[0].clear();
   st[1].clear();
   bool odds = false;
+  const u32 klane = L::rows_lane(lane), vlane = L::columns_lane(lane);
 
   if (from < end) arrive(from, lds);
   // One step; `edge`: some key may be hidden from some row of the tile.
@@ -823,19 +833,33 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
     }
     const int32_t page = table[key0 / GEN_PAGE];
     if (key0 >= hi || page < 0 || page >= c.n_pages) return;   // (the same for the whole wave)
+    typedef __attribute__((address_space(3))) const bf16 lds_bf16;
+    const u32 kat = klane + static_cast<u32>(reinterpret_cast<uintptr_t>((lds_bf16*)tk));
+    const u32 vat = vlane + static_cast<u32>(reinterpret_cast<uintptr_t>((lds_bf16*)tv));
     f32x4 s[2][T / 16];
 #pragma unroll
     for (int j = 0; j < T / 16; ++j) s[0][j] = s[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Fragments are read AHEAD ahead of their products: left alone, the compiler
+    // reads each into the same registers and waits for it, the whole LDS latency
+    // for every two products (2,000 new rows on 3 prompts of 14k: 407 us, 390 so,
+    // with 2 to 4)
+    constexpr int NK = NS * (T / 16), NV = DT * (T / 32), AHEAD = 3;
+    bf16x8 kf[NK], vf[NV];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) kf[n] = L::rows(kat, n / NS, n % NS);
+    __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);           // the SIMD's other waves do their softmax meanwhile
 #pragma unroll
-    for (int d = 0; d < NS; ++d)
-#pragma unroll
-      for (int j = 0; j < T / 16; ++j) {
-        const bf16x8 kf = L::rows(tk, 16 * j, d, lane);
-        s[0][j] = mfma32(kf, qf[0][d], s[0][j]);
-        s[1][j] = mfma32(kf, qf[1][d], s[1][j]);
-      }
+    for (int n = 0; n < NK; ++n) {
+      if (n + AHEAD < NK) kf[n + AHEAD] = L::rows(kat, (n + AHEAD) / NS, (n + AHEAD) % NS);
+      s[0][n / NS] = mfma32(kf[n], qf[0][n % NS], s[0][n / NS]);
+      s[1][n / NS] = mfma32(kf[n], qf[1][n % NS], s[1][n / NS]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
     __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) vf[n] = L::columns(vat, n / DT, n % DT);
+    __builtin_amdgcn_sched_barrier(0);
     const int32_t lim[2] = {edge ? reach.of(place_of(A, stacked_of(0))) : 0,
                             edge ? reach.of(place_of(A, stacked_of(1))) : 0};
     float top[2];
@@ -870,31 +894,32 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
         }
     }
     u32 odd = 0;
+    bf16x8 w[T / 32][2];
 #pragma unroll
-    for (int h = 0; h < T / 32; ++h) {
-      bf16x8 w[2];
+    for (int h = 0; h < T / 32; ++h)
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
         const f32x4 &x = s[a][2 * h], &y = s[a][2 * h + 1];
-        w[a] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]),
-                                                pack_bf16(y[2], y[3])});
+        w[h][a] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]),
+                                                   pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])});
       }
-      __builtin_amdgcn_s_setprio(1);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int j = 0; j < DT; ++j) {
-        bf16x8 vf = L::columns(tv, 32 * h, 16 * j, lane);
-        if constexpr (edge) {
-          u32x4 f = __builtin_bit_cast(u32x4, vf);
+    for (int n = 0; n < NV; ++n) {
+      if (n + AHEAD < NV) vf[n + AHEAD] = L::columns(vat, (n + AHEAD) / DT, (n + AHEAD) % DT);
+      const int j = n % DT;
+      if constexpr (edge) {
+        u32x4 f = __builtin_bit_cast(u32x4, vf[n]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) f[e] = finite_pair(f[e], odd);
-          vf = __builtin_bit_cast(bf16x8, f);
-        }
-        st[0].acc[j] = mfma32(vf, w[0], st[0].acc[j]);
-        st[1].acc[j] = mfma32(vf, w[1], st[1].acc[j]);
-        if constexpr (edge) __builtin_amdgcn_sched_barrier(0);   // (one fragment's registers at a time)
+        for (int e = 0; e < 4; ++e) f[e] = finite_pair(f[e], odd);
+        vf[n] = __builtin_bit_cast(bf16x8, f);
       }
-      __builtin_amdgcn_s_setprio(0);
+      st[0].acc[j] = mfma32(vf[n], w[n / DT][0], st[0].acc[j]);
+      st[1].acc[j] = mfma32(vf[n], w[n / DT][1], st[1].acc[j]);
+      __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
     if constexpr (edge) odds |= __any(odd != 0);
   };
   const int32_t mid = min(end, max(from, lo / T));
@@ -939,7 +964,7 @@ template <int D, bool E4M3>
 __global__ __launch_bounds__(GEN_THR, 3) void k_gen_attn(GenArgs A) {
   constexpr int TILE = gen_step<D>() * D * 2;      // bytes
   static_assert(4 * TILE >= 2 * 64 * GEN_JOIN * 16, "a join fits");
-  __shared__ __align__(16) char lds[E4M3 ? 5 * TILE : 4 * TILE];
+  __shared__ __align__(256) char lds[E4M3 ? 5 * TILE : 4 * TILE];   // (rows of 256 bytes, see GenTile)
   const int item = static_cast<int>(A.c.by_heads.div(blockIdx.x)), hk = blockIdx.x - item * A.c.H;
   const Scalars it = scalars(A.items) + static_cast<int64_t>(item) * GI_WORDS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
