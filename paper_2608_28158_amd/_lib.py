@@ -263,6 +263,7 @@ def rollout_binding():
     library), bound to the loaded library's functions."""
     global _binding
     if _binding is None:
+        import torch  # noqa: F401  (whose libraries the binding needs)
         L = rollout()
         try:
             from . import _rollout as ext

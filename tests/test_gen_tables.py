@@ -222,6 +222,24 @@ def test_steps_refuse(L):
     assert call(True, beta=None) == E
 
 
+def test_python_calls_refuse_tensors_of_the_cpu(L):
+    import torch
+    from paper_2608_28158_amd.rollout import RolloutCache, kda_step, la_step
+    x, g, S = torch.zeros(1, 2, 64), torch.zeros(1, 2), torch.zeros(1, 2, 64, 64)
+    with pytest.raises(RuntimeError, match="GPU only"):
+        la_step(x, x, x, g, S)
+    with pytest.raises(RuntimeError, match="GPU only"):
+        kda_step(x, x, x, x, g, S)
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        la_step(x.double(), x, x, g, S)
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        la_step(x[0], x, x, g, S)
+    with pytest.raises(TypeError):
+        la_step(None, x, x, g, S)
+    with pytest.raises(RuntimeError, match="GPU only"):
+        RolloutCache(2, 2, 1, 2, 64, device="cpu")
+
+
 # ---------------------------------------------------------------------------
 # the oracle's rounding, against every code
 # ---------------------------------------------------------------------------
