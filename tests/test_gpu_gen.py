@@ -196,10 +196,10 @@ def compare(o, lse, ref, d):
     tol_o, tol_l = bounds(ro, mag, reach, rl, d)
     got, gl = f64(o), f64(lse)
     assert np.all(np.isfinite(got))
-    empty = ~np.isfinite(rl)
-    assert np.all(gl[empty] == -np.inf) and not got[empty].any()
+    some = np.isfinite(rl)
+    assert np.all(gl[~some] == -np.inf) and not got[~some].any()
     assert np.all(np.abs(got - ro) <= tol_o), np.max(np.abs(got - ro) / np.maximum(tol_o, 1e-30))
-    assert np.all(np.abs(gl - rl)[~empty] <= tol_l[~empty]), np.max((np.abs(gl - rl) / tol_l)[~empty])
+    assert np.all(np.abs(gl[some] - rl[some]) <= tol_l[some]), np.max(np.abs(gl[some] - rl[some]) / tol_l[some])
 
 
 # parents, rows, new rows
