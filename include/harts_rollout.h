@@ -84,8 +84,7 @@ int harts_cache_read(const harts_cache* cache, const int32_t* rows, int64_t n, v
  *            first stacked row, stacked rows, split, splits, new rows of the
  *            segment, part of a row's first part, 16-row tiles of a wave,
  *            waves along rows, multiplier and shift that divide by splits); a
- *            stacked row is one of the Hq/Hkv
- *            query heads of one query row.
+ *            stacked row is one of the Hq/Hkv query heads of one query row.
  *   part_off [n_rows + 1] out: partial results of every row (in q's order).
  *   Errors: HARTS_EINVAL (NULL, sizes, a parent out of range or a cycle),
  *   HARTS_EUNSUPPORTED (table sizes beyond int32), HARTS_ENOMEM.
@@ -97,7 +96,7 @@ int harts_cache_read(const harts_cache* cache, const int32_t* rows, int64_t n, v
  *   not see has no influence on it, whatever its values.  Deterministic.
  * All: HARTS_EINVAL (NULL, misaligned, small workspace), HARTS_EUNSUPPORTED
  * (d, heads, kind), HARTS_EHIP.  Device calls are asynchronous and can be
- * captured; o must not overlap q.
+ * captured; o, lse and ws overlap no other argument.
  * ---------------------------------------------------------------------- */
 typedef struct harts_gen_sizes {
   int64_t n_rows, n_items, n_parts, n_join; /* n_join: rows of several parts */
@@ -132,13 +131,13 @@ int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* sizes, const
  *               [0, n_out) the last state is not kept.  Where an index of
  *               idx_out repeats an earlier one, that sequence writes no
  *               state and its outputs are NaN.
- *   S_out may be S_in itself if idx_out is idx_in (and n_out n_in), for an
+ *   S_out may be S_in itself if idx_out is idx_in and n_out = n_in, for an
  *   update in place; otherwise the two must not overlap.
  * Rows behind the last sequence, entries that no index names and outputs of
  * sequences without rows stay as they are; a sequence without rows hands its
  * state on.  dtype HARTS_BF16 or HARTS_F32, d in {64, 128}.  Row offsets are
- * clamped to [0, n_rows] and must not decrease; o overlaps no input.
- * Deterministic.  Errors as above.
+ * clamped to [0, n_rows] and must not decrease.  o and S_out overlap no other
+ * argument, except S_out and S_in as above.  Deterministic.  Errors as above.
  * ---------------------------------------------------------------------- */
 int harts_la_step(int32_t dtype, int64_t n_seq, int64_t n_rows, int32_t H, int32_t d, float scale, const void* q,
                   const void* k, const void* v, const float* g, const int32_t* row_off, const float* S_in,

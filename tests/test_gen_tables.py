@@ -214,6 +214,8 @@ def test_steps_refuse(L):
         assert call(kda, q=None) == E and call(kda, o=None) == E and call(kda, S=None) == E and call(kda, So=None) == E
         assert call(kda, q=P + 8) == E and call(kda, S=16 * P + 4) == E
         assert call(kda, o=P) == E and call(kda, o=3 * P + 16) == E                # o over an input
+        assert call(kda, o=4 * P) == E and call(kda, o=16 * P) == E and call(kda, o=32 * P) == E
+        assert call(kda, So=2 * P) == E and call(kda, So=4 * P) == E               # S_out over k, g
         assert call(kda, So=16 * P, ii=P, io=2 * P) == E                           # in place, two indexes
         assert call(kda, So=16 * P, n_out=1) == E                                  # in place, two sizes
         assert call(kda, So=16 * P + 16) == E                                      # overlap
