@@ -49,7 +49,7 @@ Shape shape_of(int64_t m, int64_t cap) {
   return {2, 4};
 }
 
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }   // (a up to 2^63 - 1)
 
 int make(const char* where, int32_t n_seg, const int32_t* parent, const int32_t* n_new, const int64_t* cap, int32_t Hq,
          int32_t Hkv, GenPlan& P) {

@@ -101,6 +101,14 @@ def test_a_deep_chain_and_many_segments(L):
     assert sz.n_items == n and sz.n_join == 0
 
 
+def test_the_largest_capacity(L):
+    """A capacity is a hint, up to the type's largest: the most splits, not none."""
+    top = np.iinfo(np.int64).max
+    sz, _, _, items, off = tables(L, [-1, 0], [0, 3], [top, 40], 2, 1)
+    assert sz.n_items == 4097 and list(off) == [0, 4097, 2 * 4097, 3 * 4097]
+    assert sorted(items[items[:, 0] == 0][:, 4]) == list(range(4096))
+
+
 def test_no_rows(L):
     from paper_2608_28158_amd import _lib
     sz, rows, order, items, off = tables(L, [-1, 0], [0, 0], [10, 10], 4, 4)
