@@ -140,7 +140,10 @@ Tensor step(bool kda, const Tensor& q, const Tensor& k, const Tensor& v, const T
   if (out) check("out", *out, type, {n_rows, H, d});
   if (kda) check("g", g, at::kFloat, {n_rows, H, d});
   else check("g", g, at::kFloat, {n_rows, H});
-  if (kda) check("beta", *beta, at::kFloat, {n_rows, H});
+  if (kda) {
+    if (!beta) throw py::value_error("beta must be float32 [rows, H], got None");
+    check("beta", *beta, at::kFloat, {n_rows, H});
+  }
   int64_t n_seq = n_rows;
   if (row_off) {
     n_seq = row_off->numel() - 1;

@@ -247,6 +247,11 @@ def test_refusals():
                dict(S=S, row_off=torch.tensor([0, 2], dtype=torch.int32))):
         with pytest.raises(ValueError):
             call(False, x, **kw)
+    with pytest.raises(ValueError, match="beta"):
+        call(True, {**x, "g": x["q"].float(), "beta": S.new_empty(0)}, S=S)
+    from paper_2608_28158_amd.rollout import kda_step
+    with pytest.raises(ValueError, match="beta"):
+        kda_step(*(x[n].cuda() for n in "qkv"), x["q"].float().cuda(), None, S)
     with pytest.raises(RuntimeError):
         call(False, {**x, "v": x["v"].cuda().requires_grad_()}, S=S)
     with pytest.raises(ValueError):
