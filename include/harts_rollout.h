@@ -43,7 +43,8 @@ enum { HARTS_E4M3 = 2 }; /* 8-bit cache storage, beside HARTS_BF16 */
  *   given or, for e4m3, each (row, head) with the smallest scale 2^e
  *   (e >= -126) that brings its largest finite magnitude to 448 or less,
  *   every x * 2^-e rounded once to nearest even (infinities and NaN are
- *   stored as NaN).  A call may name a row only once.
+ *   stored as NaN).  A call may name a row only once; k_new and v_new lie
+ *   outside the cache.
  * harts_cache_read -- k_out, v_out [n][H][d] bf16: the values that the rows
  *   stand for, exact (an e4m3 code has 4 significant bits).
  * ---------------------------------------------------------------------- */
