@@ -26,7 +26,8 @@ enum { HARTS_E4M3 = 2 }; /* 8-bit cache storage, beside HARTS_BF16 */
  *   k, v       [n_pages][H][64][d]: bf16 (kind HARTS_BF16) or e4m3 codes
  *              (HARTS_E4M3).  16-byte aligned.
  *   k_exp, v_exp  [n_pages][H][64] biased scale exponents of e4m3 rows: a
- *              stored code y with exponent b stands for y * 2^(b - 127).
+ *              stored code y with exponent b in [1, 254] stands for
+ *              y * 2^(b - 127), for an infinity past what bf16 holds.
  *              4-byte aligned; NULL for bf16.
  *   pages      [n_seg][pitch] int32 page of every 64 rows, -1 for none.
  *   len        [n_seg] int32 rows of every segment, new rows included.
@@ -43,8 +44,9 @@ enum { HARTS_E4M3 = 2 }; /* 8-bit cache storage, beside HARTS_BF16 */
  *   given or, for e4m3, each (row, head) with the smallest scale 2^e
  *   (e >= -126) that brings its largest finite magnitude to 448 or less,
  *   every x * 2^-e rounded once to nearest even (infinities and NaN are
- *   stored as NaN).  A call may name a row only once; k_new and v_new lie
- *   outside the cache.
+ *   stored as NaN; where the nearest code stands for 2^128, which bf16 does
+ *   not hold, from 248 * 2^120, the one below, 240 * 2^120, is taken).  A call
+ *   may name a row only once; k_new and v_new lie outside the cache.
  * harts_cache_read -- k_out, v_out [n][H][d] bf16: the values that the rows
  *   stand for, exact (an e4m3 code has 4 significant bits).
  * ---------------------------------------------------------------------- */

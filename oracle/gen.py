@@ -27,13 +27,16 @@ def e4m3_round(y):
 
 
 def e4m3_vectors(x):
-    """(values that the stored vectors stand for, scale exponents) of x [..., d]."""
+    """(values that the stored vectors stand for, scale exponents) of x [..., d].
+    The values are bf16: 2^128, which the largest finite ones would round to, is
+    past its range, and 240 x 2^120 is the largest that a code stands for."""
     x = np.asarray(x, np.float64)
     fin = np.isfinite(x)
     top = np.max(np.abs(np.where(fin, x, 0.0)), axis=-1)
     e = np.vectorize(e4m3_scale, otypes=[np.int64])(top)
     s = np.exp2(e.astype(np.float64))[..., None]
-    return np.where(fin, e4m3_round(np.where(fin, x, 0.0) / s) * s, np.nan), e
+    most = 240 * 2.0 ** 120
+    return np.where(fin, np.clip(e4m3_round(np.where(fin, x, 0.0) / s) * s, -most, most), np.nan), e
 
 
 def chain(parent, s):

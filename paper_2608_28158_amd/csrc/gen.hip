@@ -96,7 +96,9 @@ __device__ inline float exp_scale(u32 b) { return __builtin_bit_cast(float, b <<
 // Eight bf16 as e4m3 codes with the scale exponent of the D / 8 lanes that hold
 // the row: the smallest e >= -126 with max <= 448 2^e.  448 = 1.75 2^8, so e is
 // the maximum's exponent less 8, one more where its significand exceeds 1.75.
-// x 2^-e is exact in float32 and at most 448: one rounding, no saturation.
+// x 2^-e is exact in float32 (or so small that its code is 0) and at most 448: one
+// rounding.  Only at the largest scale, 2^120, does a code stand for more than
+// bf16 holds: 256 and up, the nearest to 248 and more.  Those take 240.
 template <int LANES>
 __device__ inline u32x2 quantise(const u32x4& x, u32& exponent) {
   u32 top = 0;
@@ -114,14 +116,14 @@ __device__ inline u32x2 quantise(const u32x4& x, u32& exponent) {
   }
   const int b = static_cast<int>(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
   exponent = b < 1 ? 1u : static_cast<u32>(b);
-  const float inv = exp_scale(254u - exponent);
+  const float inv = exp_scale(254u - exponent), most = exponent == 247u ? 240.f : 448.f;
   float f[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32 bits = ((x[i] >> (16 * h)) & 0xffffu) << 16;
-      const float y = __builtin_bit_cast(float, bits) * inv;
+      const float y = __builtin_amdgcn_fmed3f(__builtin_bit_cast(float, bits) * inv, -most, most);
       f[2 * i + h] = (bits & 0x7f800000u) == 0x7f800000u ? __builtin_nanf("") : y;
     }
   u32x2 out;
@@ -449,7 +451,8 @@ __device__ inline void add_odd(const CacheView& c, Scalars table, int hk, int32_
     for (int j = c0; j < c0 + cols; ++j) {
       const int64_t at = (row0 + k) * D + j;
       float x;
-      if constexpr (E4M3) x = (reinterpret_cast<const uint8_t*>(c.v)[at] & 0x7fu) == 0x7fu ? __builtin_nanf("") : 0.f;
+      if constexpr (E4M3)      // (codes that a caller wrote itself may stand for more than bf16 holds)
+        x = __builtin_bit_cast(float, dequantise(reinterpret_cast<const uint8_t*>(c.v)[at], exp_scale(c.ve[row0 + k]))[0] << 16);
       else x = static_cast<float>(reinterpret_cast<const bf16*>(c.v)[at]);
       if (!(fabsf(x) < INFINITY)) out[j] = static_cast<T>(static_cast<float>(out[j]) + x);
     }

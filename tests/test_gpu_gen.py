@@ -541,3 +541,78 @@ def test_refusals():
     q = torch.zeros((1, 4, 64), dtype=torch.bfloat16, device="cuda")
     with pytest.raises(_lib.HartsError):
         b.attend(q, out=q)
+
+
+# ---------------------------------------------------------------------------
+# the ends of the types' ranges
+# ---------------------------------------------------------------------------
+
+TOP = 2.0 ** 120
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_e4m3_of_the_largest_values(d):
+    """The nearest code of 248 x 2^120 and more stands for 2^128, which bf16 does not hold: they take
+    the largest one that it does, 240 x 2^120."""
+    x, want = np.zeros((4, 1, d)), np.zeros((4, 1, d))
+    x[0, 0, :6] = [255, -248, 247, 240, -232, 1]            # (232 and 216 lie half way between two codes)
+    want[0, 0, :6] = [240, -240, 240, 240, -224, 1]
+    x[1, 0, :4] = [-225, 216, 129, np.nan]
+    want[1, 0, :4] = [-224, 224, 128, np.nan]
+    x[2, 0, :2] = [224, -223]                                # a scale of 2^119: codes of 448 and less
+    want[2, 0, :2] = [224, -224]
+    x[3] = 255
+    want[3] = 240
+    b = bf16_values(x * TOP)
+    assert np.array_equal(f64(b), x * TOP, equal_nan=True)
+    assert np.array_equal(e4m3_vectors(f64(b))[0], want * TOP, equal_nan=True)
+    c = new_cache(1, 1, 1, 1, d, "e4m3")
+    c.reserve(0, 4)
+    c.len[0] = 4
+    rows = table([(0, i) for i in range(4)])
+    c.write(rows, b.cuda(), b.flip(0).cuda())
+    k, v = c.read(rows)
+    assert np.array_equal(f64(k), want * TOP, equal_nan=True)
+    assert np.array_equal(f64(v)[::-1], want * TOP, equal_nan=True)
+
+
+@pytest.mark.parametrize("new", [5, 35])
+@pytest.mark.parametrize("where", [(0, 10), (1, 41)])
+def test_the_largest_values_under_attention(where, new):
+    """A value near the type's largest, in a row that all queries see and in a drafted one that some see
+    (equal weights: the sum of one such value and ordinary ones is a float32)."""
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    rng = np.random.default_rng(14)
+    d, parent, lens = 64, [-1, 0], [70, 70]
+    c, K, V = filled(parent, lens, 2, d, "e4m3", rng)
+    k, v = c.read(table([where]))
+    v[0, 1, 3:9] = 255 * TOP
+    c.write(table([where]), k, v)
+    V[where[0]][where[1]] = e4m3_vectors(f64(v))[0][0]
+    assert np.isfinite(V[where[0]]).all() and V[where[0]].max() == 240 * TOP
+    q = torch.zeros((new, 4, d), dtype=torch.bfloat16)
+    o, lse = RolloutBatch(c, parent, [0, new], 4, capacity=lens).attend(q.cuda())
+    ref = forest_decode(parent, [0, new], K, V, f64(q), 0.125)
+    compare(o, lse, ref, d)
+
+
+@pytest.mark.parametrize("new", [5, 35])
+def test_codes_beyond_bf16(new):
+    """Codes that a caller lays into the cache itself and that stand for more than bf16 holds are
+    infinities: for the rows that see them, and for no other."""
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    rng = np.random.default_rng(15)
+    d, parent, lens = 64, [-1, 0], [70, 70]
+    c, K, V = filled(parent, lens, 2, d, "e4m3", rng)
+    at = 70 - new + 3                                        # the fourth of the new rows
+    page, slot = int(c.pages[1, at // 64]), at % 64
+    c.v.view(torch.uint8)[0, page, 1, slot] = 0x7e           # 448
+    c.v_exp[0, page, 1, slot] = 254                          # x 2^127
+    assert torch.isinf(c.read(table([(1, at)]))[1][0, 1]).all()
+    q = bf16_values(rng.standard_normal((new, 4, d)))
+    o, lse = RolloutBatch(c, parent, [0, new], 4, capacity=lens).attend(q.cuda())
+    ref = forest_decode(parent, [0, new], K, V, f64(q), 0.125)
+    compare(o[:3], lse[:3], [x[:3] for x in ref], d)
+    got = f64(o)
+    assert np.all(got[3:, 2:] == np.inf)
+    assert np.all(np.abs(got[:, :2] - ref[0][:, :2]) <= bounds(ref[0], ref[2], ref[3], ref[1], d)[0][:, :2])
