@@ -616,6 +616,7 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
 
   if (parts == 1) {
     const int64_t rh = static_cast<int64_t>(row) * A.Hq + head;
+    if (st.sum == 0.f) st.clear();                  // (no weight at all: not 0 times an infinite value)
     const float f = st.sum == 0.f ? 0.f : 1.f / st.sum;
     u32 out[D / 8];
 #pragma unroll
@@ -627,7 +628,7 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) op[e] = u32x4{out[4 * e], out[4 * e + 1], out[4 * e + 2], out[4 * e + 3]};
     if (A.lse && g == 0) A.lse[rh] = log_sum(st.ref, st.sum);
-    if (odds)
+    if (odds && st.sum != 0.f)
       for (u = max(from, lo / T); u < end; ++u)
         add_odd<D, E4M3>(c, table, hk, u * T, T, n, lim, A.o + rh * D, g * (D / 4), D / 4);
   } else {
@@ -939,11 +940,12 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
     const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
     if (parts == 1) {
       const int64_t rh = static_cast<int64_t>(row) * A.Hq + head;
+      if (st[a].sum == 0.f) st[a].clear();     // (as in gen_few)
       const float f = st[a].sum == 0.f ? 0.f : 1.f / st[a].sum;
 #pragma unroll
       for (int j = 0; j < DT; ++j) Vec4<bf16>::store(A.o + rh * D + 16 * j + 4 * g, st[a].acc[j] * f);
       if (A.lse && g == 0) A.lse[rh] = log_sum(st[a].ref, st[a].sum);
-      if (odds)
+      if (odds && st[a].sum != 0.f)
         for (int32_t u = mid; u < end; ++u)
           for (int j = 0; j < DT; ++j)
             add_odd<D, E4M3>(c, table, hk, u * T, T, n, lim, A.o + rh * D, 16 * j + 4 * g, 4);
@@ -1043,6 +1045,7 @@ __global__ __launch_bounds__(GEN_THR) void k_gen_join(GenArgs A, int64_t n) {
     }
   }
   if (parts <= 1) return;
+  if (sum == 0.f) acc = f32x4{0.f, 0.f, 0.f, 0.f};   // (as in gen_few)
   Vec4<bf16>::store(A.o + rh * D + c, acc * (sum == 0.f ? 0.f : 1.f / sum));
   if (A.lse && c == 0) A.lse[rh] = log_sum(ref, sum);
 }

@@ -616,3 +616,25 @@ def test_codes_beyond_bf16(new):
     got = f64(o)
     assert np.all(got[3:, 2:] == np.inf)
     assert np.all(np.abs(got[:, :2] - ref[0][:, :2]) <= bounds(ref[0], ref[2], ref[3], ref[1], d)[0][:, :2])
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,new", [([40], 1), ([2000], 1), ([300, 40], 3), ([300, 90], 40), ([700], 100)])
+def test_only_scores_of_minus_infinity(lens, new, d, bad):
+    """Rows whose every score is -infinity give zeros, whatever the values of those keys."""
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    parent = list(range(-1, len(lens) - 1))
+    c = new_cache(sum(-(-n // 64) for n in lens), len(lens), -(-max(lens) // 64), 1, d, "bf16")
+    for s, n in enumerate(lens):
+        c.reserve(s, n)
+        c.len[s] = n
+        k, v = (torch.zeros((n, 1, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        k[:, 0, 0] = float("-inf")
+        v[:] = bad
+        c.write(table([(s, p) for p in range(n)]), k, v)
+    q = torch.zeros((new, 2, d), dtype=torch.bfloat16, device="cuda")
+    q[:, :, 0] = 1
+    n_new = [0] * (len(lens) - 1) + [new]
+    o, lse = RolloutBatch(c, parent, n_new, 2, capacity=lens).attend(q)
+    assert not f64(o).any() and np.all(f64(lse) == -np.inf)
