@@ -126,7 +126,8 @@ int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* sizes, const
  *   harts_kda_step  D = Diag(e^{g_t}) S_{t-1},
  *                   S_t = D + beta_t k_t (v_t - D^T k_t)^T, o_t the same.
  *   q, k, v, o  [n_rows][H][d] (dtype); g float32 [n_rows][H] (la) or
- *               [n_rows][H][d] (kda); beta float32 [n_rows][H].
+ *               [n_rows][H][d] (kda); beta float32 [n_rows][H].  16-byte
+ *               aligned, as the states are; la's g and beta 4-byte aligned.
  *   S_in        float32 [n_in][H][d][d]; idx_in int32 [n_seq] or NULL (entry
  *               i).  Several sequences may start from one entry.  An index
  *               outside [0, n_in) starts from zeros.

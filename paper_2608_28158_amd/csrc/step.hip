@@ -220,7 +220,7 @@ int step(const char* where, int32_t dtype, int32_t d, const StepArgs& A, void* s
   if (A.n_rows > 0 && (!A.q || !A.k || !A.v || !A.g || !A.o || (KDA && !A.beta)))
     return fail(HARTS_EINVAL, "NULL pointer");
   if ((A.n_in > 0 && !A.S_in) || (A.n_out > 0 && !A.S_out)) return fail(HARTS_EINVAL, "NULL state pool");
-  if (!al(A.q, 16) || !al(A.k, 16) || !al(A.v, 16) || !al(A.o, 16) || !al(A.g, 16) || !al(A.beta, 4) ||
+  if (!al(A.q, 16) || !al(A.k, 16) || !al(A.v, 16) || !al(A.o, 16) || !al(A.g, KDA ? 16 : 4) || !al(A.beta, 4) ||
       !al(A.S_in, 16) || !al(A.S_out, 16) || !al(A.row_off, 4) || !al(A.idx_in, 4) || !al(A.idx_out, 4))
     return fail(HARTS_EINVAL, "misaligned pointer");
   const uintptr_t in = reinterpret_cast<uintptr_t>(A.S_in), out = reinterpret_cast<uintptr_t>(A.S_out);

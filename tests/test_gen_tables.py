@@ -232,6 +232,20 @@ def test_steps_refuse(L):
     assert call(True, beta=None) == E
 
 
+def test_gates_of_linear_attention_have_float_alignment(L):
+    """g [n_rows][H] is read one by one; only what comes after the alignment is refused here (o over k)."""
+    from paper_2608_28158_amd import _lib
+    def call(g, kda):
+        head = (_lib.HARTS_BF16, 2, 2, 5, 64, 1.0, P, 2 * P, 3 * P, g)
+        tail = (None, 16 * P, None, 2, 32 * P, None, 2, 2 * P, None)
+        rc = L.harts_kda_step(*head, 6 * P, *tail) if kda else L.harts_la_step(*head, *tail)
+        return rc, _lib.last_error()
+    for g in (4 * P + 4, 4 * P + 20, 4 * P + 8):
+        assert call(g, False) == (_lib.HARTS_EINVAL, "harts_la_step: o overlaps an input")
+        assert call(g, True) == (_lib.HARTS_EINVAL, "harts_kda_step: misaligned pointer")
+    assert call(4 * P + 2, False) == (_lib.HARTS_EINVAL, "harts_la_step: misaligned pointer")
+
+
 def test_python_calls_refuse_tensors_of_the_cpu(L):
     import torch
     from paper_2608_28158_amd.rollout import RolloutCache, kda_step, la_step

@@ -261,3 +261,19 @@ def test_refusals():
     v = x["v"].cuda()
     with pytest.raises(_lib.HartsError):
         call(False, {**x, "v": v}, S=S, out=v)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gates_of_any_float_alignment(dtype):
+    """A token's slice of gates [tokens, H], H no multiple of 4 (linear attention reads them one by one)."""
+    rng = np.random.default_rng(31)
+    H, d = 5, 64
+    x = draw(rng, 3, H, d, dtype, False, 1)
+    g = x["g"].cuda()
+    for t in range(3):
+        y = {m: (v[t:t + 1] if m != "S" else v) for m, v in x.items()}
+        y["q"], y["k"], y["v"] = (y[m].clone() for m in "qkv")
+        S = x["S"].cuda()
+        assert t == 0 or g[t:t + 1].data_ptr() % 16 != 0
+        o = call(False, {**y, "g": g[t:t + 1]}, S=S)
+        check(False, y, [0, 1], [0], o, S, [0], d ** -0.5, dtype)
