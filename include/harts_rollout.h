@@ -46,9 +46,11 @@ enum { HARTS_E4M3 = 2 }; /* 8-bit cache storage, beside HARTS_BF16 */
  *   every x * 2^-e rounded once to nearest even (infinities and NaN are
  *   stored as NaN; where the nearest code stands for 2^128, which bf16 does
  *   not hold, from 248 * 2^120, the one below, 240 * 2^120, is taken).  A call
- *   may name a row only once; k_new and v_new lie outside the cache.
+ *   may name a row only once; k_new, v_new and rows lie outside the cache,
+ *   whose parts lie apart.
  * harts_cache_read -- k_out, v_out [n][H][d] bf16: the values that the rows
- *   stand for, exact (an e4m3 code has 4 significant bits).
+ *   stand for, exact (an e4m3 code has 4 significant bits).  They overlap
+ *   no other argument.
  * ---------------------------------------------------------------------- */
 typedef struct harts_cache {
   void *k, *v;

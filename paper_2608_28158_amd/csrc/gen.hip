@@ -52,6 +52,7 @@
 #include "la_common.hpp"
 #include "lds_load.hpp"
 #include "plan.hpp"
+#include "regions.hpp"
 
 namespace harts {
 namespace {
@@ -1107,6 +1108,21 @@ uint32_t piece_blocks(int64_t n, const harts_cache* c) {
 // write 84 -> 71; the write that quantises was no faster so, at d = 64 slower).
 bool past_l2(int64_t n, const harts_cache* c) { return n * c->H * c->d * 4 > (int64_t{32} << 20); }
 
+// What a cache occupies: keys and values with their scale exponents, and its tables.
+struct CacheRegions {
+  Region k, v, ke, ve, pages, len;
+  explicit CacheRegions(const harts_cache* c) {
+    const size_t rows = static_cast<size_t>(c->n_pages) * c->H * GEN_PAGE, held = rows * c->d;
+    const bool q = c->kind == HARTS_E4M3;
+    k = {c->k, q ? held : 2 * held};
+    v = {c->v, k.bytes};
+    ke = {c->k_exp, q ? rows : 0};
+    ve = {c->v_exp, q ? rows : 0};
+    pages = {c->pages, static_cast<size_t>(c->n_seg) * c->pitch * sizeof(int32_t)};
+    len = {c->len, static_cast<size_t>(c->n_seg) * sizeof(int32_t)};
+  }
+};
+
 int check_rows(const harts_cache* c, const int32_t* rows, int64_t n, const void* k, const void* v, const char* where) {
   if (int rc = check_cache(c, where)) return rc;
   if (n < 0) { set_error(std::string(where) + ": negative row count"); return HARTS_EINVAL; }
@@ -1131,6 +1147,15 @@ extern "C" int harts_cache_write(const harts_cache* cache, const int32_t* rows, 
                                  const void* v_new, void* stream) {
   if (int rc = check_rows(cache, rows, n, k_new, v_new, "harts_cache_write")) return rc;
   if (n == 0) return HARTS_OK;
+  const CacheRegions R(cache);
+  const size_t span = static_cast<size_t>(n) * cache->H * cache->d * sizeof(bf16);
+  const Region kn{k_new, span}, vn{v_new, span}, table{rows, static_cast<size_t>(n) * 2 * sizeof(int32_t)};
+  if (overlaps_any(R.k, {kn, vn, table, R.v, R.ke, R.ve, R.pages, R.len}) ||
+      overlaps_any(R.v, {kn, vn, table, R.ke, R.ve, R.pages, R.len}) ||
+      overlaps_any(R.ke, {kn, vn, table, R.ve, R.pages, R.len}) || overlaps_any(R.ve, {kn, vn, table, R.pages, R.len})) {
+    set_error("harts_cache_write: a written part of the cache overlaps another or an input");
+    return HARTS_EINVAL;
+  }
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(piece_blocks(n, cache)), dim3(GEN_THR), 0, static_cast<hipStream_t>(stream),
                        view_of(cache), rows, n, static_cast<const u32x4*>(k_new), static_cast<const u32x4*>(v_new));
@@ -1148,6 +1173,14 @@ extern "C" int harts_cache_read(const harts_cache* cache, const int32_t* rows, i
                                 void* stream) {
   if (int rc = check_rows(cache, rows, n, k_out, v_out, "harts_cache_read")) return rc;
   if (n == 0) return HARTS_OK;
+  const CacheRegions R(cache);
+  const size_t span = static_cast<size_t>(n) * cache->H * cache->d * sizeof(bf16);
+  const Region ko{k_out, span}, vo{v_out, span}, table{rows, static_cast<size_t>(n) * 2 * sizeof(int32_t)};
+  if (overlaps_any(ko, {vo, table, R.k, R.v, R.ke, R.ve, R.pages, R.len}) ||
+      overlaps_any(vo, {table, R.k, R.v, R.ke, R.ve, R.pages, R.len})) {
+    set_error("harts_cache_read: an output overlaps another or an input");
+    return HARTS_EINVAL;
+  }
   const auto launch = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3(piece_blocks(n, cache)), dim3(GEN_THR), 0, static_cast<hipStream_t>(stream),
                        view_of(cache), rows, n, static_cast<u32x4*>(k_out), static_cast<u32x4*>(v_out));
@@ -1188,10 +1221,20 @@ extern "C" int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* s
     set_error("harts_gen_attn: NULL, misaligned or small workspace; need " + std::to_string(need) + " bytes");
     return HARTS_EINVAL;
   }
-  const size_t span = static_cast<size_t>(sizes->n_rows) * Hq * cache->d * sizeof(bf16);
-  const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(o);
-  if ((q0 < o0 ? o0 - q0 : q0 - o0) < span) {
-    set_error("harts_gen_attn: o overlaps q");
+  const CacheRegions R(cache);
+  const size_t n_rows = static_cast<size_t>(sizes->n_rows), span = n_rows * Hq * cache->d * sizeof(bf16);
+  const Region out{o, span}, sums{lse, n_rows * Hq * sizeof(float)}, parts_of{ws, need}, in{q, span};
+  const Region work{items, static_cast<size_t>(sizes->n_items) * GI_WORDS * sizeof(int32_t)};
+  const Region places{order, n_rows * sizeof(int32_t)}, offsets{part_off, (n_rows + 1) * sizeof(int32_t)};
+  const auto over_an_input = [&](const Region& x) {
+    return overlaps_any(x, {in, work, places, offsets, R.k, R.v, R.ke, R.ve, R.pages, R.len});
+  };
+  if (over_an_input(out) || over_an_input(sums) || over_an_input(parts_of)) {
+    set_error("harts_gen_attn: o, lse or the workspace overlaps an input");
+    return HARTS_EINVAL;
+  }
+  if (overlaps_any(out, {sums, parts_of}) || overlap(sums, parts_of)) {
+    set_error("harts_gen_attn: o, lse and the workspace overlap");
     return HARTS_EINVAL;
   }
   GenArgs A;

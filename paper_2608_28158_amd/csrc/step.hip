@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <initializer_list>
 #include <string>
 #include <type_traits>
 
@@ -25,6 +26,7 @@
 #include "harts_rollout.h"
 #include "la_common.hpp"
 #include "plan.hpp"
+#include "regions.hpp"
 
 namespace harts {
 namespace {
@@ -230,19 +232,14 @@ int step(const char* where, int32_t dtype, int32_t d, const StepArgs& A, void* s
     return fail(HARTS_EINVAL, "S_out overlaps S_in (an update in place has one pool and one index)");
   // (the waves of a head read the same q, k and g, and none waits for another)
   const size_t rows = static_cast<size_t>(A.n_rows) * A.H, span = rows * d * (dtype == HARTS_BF16 ? 2 : 4);
-  const auto overlap = [](const void* p, size_t np, const void* q, size_t nq) {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-    return np > 0 && nq > 0 && p && q && a < b + nq && b < a + np;
-  };
-  const struct { const void* p; size_t n; } inputs[] = {
+  const size_t seqs = static_cast<size_t>(A.n_seq) * sizeof(int32_t);
+  const Region o{A.o, span}, S_in{A.S_in, A.n_in * state}, S_out{A.S_out, A.n_out * state};
+  const std::initializer_list<Region> inputs = {
       {A.q, span}, {A.k, span}, {A.v, span}, {A.g, rows * (KDA ? d : 1) * sizeof(float)},
-      {A.beta, rows * sizeof(float)}};
-  for (const auto& x : inputs) {
-    if (overlap(A.o, span, x.p, x.n)) return fail(HARTS_EINVAL, "o overlaps an input");
-    if (overlap(A.S_out, A.n_out * state, x.p, x.n)) return fail(HARTS_EINVAL, "S_out overlaps an input");
-  }
-  if (overlap(A.o, span, A.S_in, A.n_in * state) || overlap(A.o, span, A.S_out, A.n_out * state))
-    return fail(HARTS_EINVAL, "o overlaps a state pool");
+      {A.beta, rows * sizeof(float)}, {A.row_off, seqs + sizeof(int32_t)}, {A.idx_in, seqs}, {A.idx_out, seqs}};
+  if (overlaps_any(o, inputs)) return fail(HARTS_EINVAL, "o overlaps an input");
+  if (overlaps_any(S_out, inputs)) return fail(HARTS_EINVAL, "S_out overlaps an input");
+  if (overlaps_any(o, {S_in, S_out})) return fail(HARTS_EINVAL, "o overlaps a state pool");
   const int64_t blocks = (A.n_seq * A.H * (d / ST_COLS) + ST_THR / 64 - 1) / (ST_THR / 64);
   if (A.n_seq * A.H * (d / ST_COLS) > INT32_MAX - ST_THR) return fail(HARTS_EUNSUPPORTED, "too many sequences for one call");
   // States past what the last-level cache holds are not kept in it (512 sequences,

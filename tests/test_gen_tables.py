@@ -232,6 +232,53 @@ def test_steps_refuse(L):
     assert call(True, beta=None) == E
 
 
+def test_outputs_over_other_arguments_are_refused(L):
+    """Every output of every call over every other argument, at its first bytes and at its last."""
+    from paper_2608_28158_amd import _lib
+    H, d, n = 2, 64, 3
+    held, table = {_lib.HARTS_BF16: 4 * H * 64 * d * 2, _lib.HARTS_E4M3: 4 * H * 64 * d}, 2 * 2 * 4
+    def refused(fn, sizes, written, aliasable=()):
+        at = {name: (20 + 10 * i) * P for i, name in enumerate(sizes)}
+        assert max(sizes.values()) < 10 * P
+        for w in written:
+            for other in sizes:
+                if other == w or (w, other) in aliasable:
+                    continue
+                for place in (at[other], at[other] + (sizes[other] - 1) // 16 * 16, at[other] - (sizes[w] - 1) // 16 * 16):
+                    assert fn({**at, w: place}) == _lib.HARTS_EINVAL, (w, other)
+                    assert "overlap" in _lib.last_error(), (w, other, _lib.last_error())
+
+    for kind in (_lib.HARTS_BF16, _lib.HARTS_E4M3):
+        parts = dict(k=held[kind], v=held[kind], pages=table, len=2 * 4)
+        if kind == _lib.HARTS_E4M3:
+            parts.update(k_exp=4 * H * 64, v_exp=4 * H * 64)
+        cached = [x for x in ("k", "v", "k_exp", "v_exp") if x in parts]
+        def of(at):
+            return cache(**{x: at.get(x) for x in ("k", "v", "k_exp", "v_exp", "pages", "len")}, kind=kind, H=H, d=d)
+        rows = dict(rows=n * 8, k_new=n * H * d * 2, v_new=n * H * d * 2)
+        refused(lambda at: L.harts_cache_write(C.byref(of(at)), at["rows"], n, at["k_new"], at["v_new"], None),
+                {**parts, **rows}, cached)
+        refused(lambda at: L.harts_cache_read(C.byref(of(at)), at["rows"], n, at["k_new"], at["v_new"], None),
+                {**parts, **rows}, ["k_new", "v_new"])
+        sz = _lib.GenSizes(n, 5, 8, 2)
+        ws = 8 * 4 * (d + 2) * 4
+        refused(lambda at: L.harts_gen_attn(C.byref(of(at)), C.byref(sz), at["items"], at["order"], at["off"], 4, 1.0,
+                                            at["q"], at["o"], at["lse"], at["ws"], ws, None),
+                {**parts, "items": 5 * 48, "order": n * 4, "off": (n + 1) * 4, "q": n * 4 * d * 2, "o": n * 4 * d * 2,
+                 "lse": n * 4 * 4, "ws": ws}, ["o", "lse", "ws"])
+    for kda in (False, True):
+        state = H * d * d * 4
+        x = dict(q=n * H * d * 2, k=n * H * d * 2, v=n * H * d * 2, g=n * H * 4 * (d if kda else 1), off=3 * 4, S=2 * state,
+                 ii=2 * 4, So=2 * state, io=2 * 4, o=n * H * d * 2)
+        if kda:
+            x["beta"] = n * H * 4
+        def step(at):
+            head = (_lib.HARTS_BF16, 2, n, H, d, 1.0, at["q"], at["k"], at["v"], at["g"])
+            tail = (at["off"], at["S"], at["ii"], 2, at["So"], at["io"], 2, at["o"], None)
+            return L.harts_kda_step(*head, at["beta"], *tail) if kda else L.harts_la_step(*head, *tail)
+        refused(step, x, ["o", "So"])
+
+
 def test_gates_of_linear_attention_have_float_alignment(L):
     """g [n_rows][H] is read one by one; only what comes after the alignment is refused here (o over k)."""
     from paper_2608_28158_amd import _lib
