@@ -6,8 +6,8 @@
 // address (bind), so that it is the one library that the package has loaded.
 #include <ATen/Functions.h>
 #include <ATen/core/Tensor.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
-#include <c10/core/GradMode.h>
 #include <pybind11/pybind11.h>
 #include <torch/csrc/utils/pybind.h>
 
@@ -49,14 +49,16 @@ void ok(int code, const char* where) {
   if (code != HARTS_OK) (*L.fail)(code, where);
 }
 
-// Tensors on one GPU, contiguous, of a given type and shape, none recording a gradient.
+// Tensors on one GPU, contiguous, of a given type and shape, none recording a
+// gradient or carrying a tangent while those are on.
 struct Checker {
   c10::Device device;
-  bool grad;
-  explicit Checker(const Tensor& first) : device(first.device()), grad(c10::GradMode::is_enabled()) {
+  bool grad = c10::AutogradState::get_tls_state().get_grad_mode();
+  bool tangents = c10::AutogradState::get_tls_state().get_fw_grad_mode();
+  explicit Checker(const Tensor& first) : device(first.device()) {
     if (!device.is_cuda()) throw std::runtime_error("generation runs on the GPU only");
   }
-  Checker(int64_t index) : device(at::kCUDA, static_cast<c10::DeviceIndex>(index)), grad(c10::GradMode::is_enabled()) {}
+  explicit Checker(int64_t index) : device(at::kCUDA, static_cast<c10::DeviceIndex>(index)) {}
   void operator()(const char* name, const Tensor& t, at::ScalarType type, at::IntArrayRef shape) const {
     if (t.scalar_type() != type || t.sizes() != shape || !t.is_contiguous()) {
       std::ostringstream s;
@@ -71,6 +73,8 @@ struct Checker {
     }
     if (grad && t.requires_grad())
       throw std::runtime_error(std::string(name) + " requires a gradient; generation is not differentiable");
+    if (tangents && t._fw_grad(0).defined())
+      throw std::runtime_error(std::string(name) + " carries a tangent; generation is not differentiable");
   }
 };
 

@@ -20,7 +20,8 @@ cache's; a fork of a sequence is two new segments below it, with no row copied.
 A batch's tables serve every step until the forest or n_new changes, so a step
 can be captured into a graph and replayed while the lengths grow.  Nothing here
 is differentiable: inputs that require a gradient are refused while gradients
-are recorded (the training forms are tree_la, KdaRunner and harts_attn_*).
+are recorded, and inputs that carry a tangent (the training forms are tree_la,
+KdaRunner and harts_attn_*).
 """
 from __future__ import annotations
 

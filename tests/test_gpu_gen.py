@@ -638,3 +638,22 @@ def test_only_scores_of_minus_infinity(lens, new, d, bad):
     n_new = [0] * (len(lens) - 1) + [new]
     o, lse = RolloutBatch(c, parent, n_new, 2, capacity=lens).attend(q)
     assert not f64(o).any() and np.all(f64(lse) == -np.inf)
+
+
+def test_tangents_are_refused():
+    import torch.autograd.forward_ad as fwd
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    c = new_cache(2, 1, 1, 2, 64, "bf16")
+    c.reserve(0, 3)
+    c.len[0] = 3
+    x = torch.ones((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    rows = table([(0, i) for i in range(3)])
+    batch = RolloutBatch(c, [-1], [3], 2)
+    with fwd.dual_level():
+        dual = fwd.make_dual(x, torch.ones_like(x))
+        with pytest.raises(RuntimeError, match="not differentiable"):
+            c.write(rows, dual, x)
+        with pytest.raises(RuntimeError, match="not differentiable"):
+            batch.attend(dual)
+        c.write(rows, x, x)
+        batch.attend(x)

@@ -277,3 +277,17 @@ def test_gates_of_any_float_alignment(dtype):
         assert t == 0 or g[t:t + 1].data_ptr() % 16 != 0
         o = call(False, {**y, "g": g[t:t + 1]}, S=S)
         check(False, y, [0, 1], [0], o, S, [0], d ** -0.5, dtype)
+
+
+@pytest.mark.parametrize("kda", [False, True])
+def test_tangents_are_refused(kda):
+    import torch.autograd.forward_ad as fwd
+    x = draw(np.random.default_rng(33), 2, 2, 64, "f32", kda, 2)
+    S = x["S"].cuda()
+    with fwd.dual_level():
+        v = x["v"].cuda()
+        with pytest.raises(RuntimeError, match="not differentiable"):
+            call(kda, {**x, "v": fwd.make_dual(v, torch.ones_like(v))}, S=S)
+        with pytest.raises(RuntimeError, match="not differentiable"):
+            call(kda, x, S=fwd.make_dual(S, torch.ones_like(S)))
+        call(kda, x, S=S)
