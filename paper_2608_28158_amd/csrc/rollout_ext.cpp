@@ -78,12 +78,19 @@ struct Checker {
   }
 };
 
+// A tensor that a call has written counts as modified, for a backward pass that saved it.
+void written(const Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 void* ptr(const OptTensor& t) { return t ? t->data_ptr() : nullptr; }
 const int32_t* ints(const OptTensor& t) { return static_cast<const int32_t*>(ptr(t)); }
 
 const harts_cache* cache_at(uintptr_t p) { return reinterpret_cast<const harts_cache*>(p); }
 
-void cache_write(uintptr_t desc, int64_t device, uintptr_t stream, const Tensor& rows, const Tensor& k, const Tensor& v) {
+// cells: the tensors that hold the cache
+void cache_write(uintptr_t desc, int64_t device, uintptr_t stream, const py::tuple& cells, const Tensor& rows,
+                 const Tensor& k, const Tensor& v) {
   const harts_cache* c = cache_at(desc);
   const Checker check(device);
   const int64_t n = rows.dim() > 0 ? rows.size(0) : 0;
@@ -93,6 +100,7 @@ void cache_write(uintptr_t desc, int64_t device, uintptr_t stream, const Tensor&
   const c10::DeviceGuard on(check.device);
   ok(L.cache_write(c, rows.const_data_ptr<int32_t>(), n, k.const_data_ptr(), v.const_data_ptr(),
                    reinterpret_cast<void*>(stream)), "harts_cache_write");
+  for (const py::handle t : cells) written(t.cast<Tensor>());
 }
 
 py::tuple cache_read(uintptr_t desc, int64_t device, uintptr_t stream, const Tensor& rows) {
@@ -126,6 +134,7 @@ py::tuple attend(uintptr_t desc, uintptr_t sizes_at, uintptr_t items, uintptr_t 
                 static_cast<float>(scale ? *scale : 1.0 / std::sqrt(static_cast<double>(c->d))), q.const_data_ptr(),
                 o.data_ptr(), lse.data_ptr<float>(), ws_bytes > 0 ? ws.data_ptr() : nullptr,
                 static_cast<size_t>(ws_bytes), reinterpret_cast<void*>(stream)), "harts_gen_attn");
+  if (out) written(o);
   return py::make_tuple(o, lse);
 }
 
@@ -185,6 +194,8 @@ Tensor step(bool kda, const Tensor& q, const Tensor& k, const Tensor& v, const T
                  k.const_data_ptr(), v.const_data_ptr(), g.const_data_ptr<float>(), ints(row_off),
                  S.const_data_ptr<float>(), ints(idx_in), n_in, S_out.data_ptr<float>(), ints(idx_out), n_out,
                  o.data_ptr(), stream), "harts_la_step");
+  written(S_out);
+  if (out) written(o);
   return o;
 }
 

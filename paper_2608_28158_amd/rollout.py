@@ -21,7 +21,7 @@ A batch's tables serve every step until the forest or n_new changes, so a step
 can be captured into a graph and replayed while the lengths grow.  Nothing here
 is differentiable: inputs that require a gradient are refused while gradients
 are recorded, and inputs that carry a tangent (the training forms are tree_la,
-KdaRunner and harts_attn_*).
+KdaRunner and harts_attn_*).  What a call writes counts as modified.
 """
 from __future__ import annotations
 
@@ -83,6 +83,7 @@ class RolloutCache:
         self._layers = [_lib.Cache(*(ptr(t, i) for t in (self.k, self.v, self.k_exp, self.v_exp)), *fixed)
                         for i in range(layers)]
         self._desc = [C.addressof(c) for c in self._layers]
+        self._cells = tuple(t for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None)
 
     # -- pages (host bookkeeping) --------------------------------------------
     @property
@@ -128,7 +129,7 @@ class RolloutCache:
         (int32 segment and position, negative from the segment's end).  A row
         may be named once; entries that name no existing row are skipped."""
         index = self.device.index
-        self._ext.cache_write(self.desc(layer), index, _raw_stream(index), rows, k, v)
+        self._ext.cache_write(self.desc(layer), index, _raw_stream(index), self._cells, rows, k, v)
 
     def read(self, rows, layer: int = 0):
         """(k, v) [n, heads, d] bf16: what the rows stand for, zeros where an

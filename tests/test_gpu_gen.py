@@ -640,6 +640,32 @@ def test_only_scores_of_minus_infinity(lens, new, d, bad):
     assert not f64(o).any() and np.all(f64(lse) == -np.inf)
 
 
+# ---------------------------------------------------------------------------
+# autograd, streams, hints
+# ---------------------------------------------------------------------------
+
+# ---------------------------------------------------------------------------
+# autograd
+# ---------------------------------------------------------------------------
+
+def test_writes_are_seen_by_autograd():
+    """Tensors that a call writes count as modified: a backward pass that saved one refuses to use it."""
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    c = new_cache(2, 1, 1, 2, 64, "e4m3")
+    c.reserve(0, 3)
+    c.len[0] = 3
+    x = torch.ones((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    before = [t._version for t in (c.k, c.v, c.k_exp, c.v_exp)]
+    c.write(table([(0, i) for i in range(3)]), x, x)
+    assert all(t._version > b for t, b in zip((c.k, c.v, c.k_exp, c.v_exp), before))
+    w = torch.ones((3, 2, 64), dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    out = torch.ones_like(x)
+    y = (w * out).sum()
+    RolloutBatch(c, [-1], [3], 2).attend(x, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.backward()
+
+
 def test_tangents_are_refused():
     import torch.autograd.forward_ad as fwd
     from paper_2608_28158_amd.rollout import RolloutBatch
@@ -657,3 +683,18 @@ def test_tangents_are_refused():
             batch.attend(dual)
         c.write(rows, x, x)
         batch.attend(x)
+
+
+def test_inference_tensors_are_written():
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    with torch.inference_mode():
+        c = new_cache(2, 1, 1, 2, 64, "bf16")
+        c.reserve(0, 3)
+        c.len[0] = 3
+        out = torch.empty((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    x = torch.ones((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    for mode in (torch.inference_mode(), torch.no_grad()):
+        with mode:
+            c.write(table([(0, i) for i in range(3)]), x, x)
+            RolloutBatch(c, [-1], [3], 2).attend(x, out=out)
+            assert torch.all(out == 1)

@@ -280,6 +280,25 @@ def test_gates_of_any_float_alignment(dtype):
 
 
 @pytest.mark.parametrize("kda", [False, True])
+def test_writes_are_seen_by_autograd(kda):
+    x = draw(np.random.default_rng(32), 2, 2, 64, "f32", kda, 2)
+    w = torch.ones((2, 2, 64), device="cuda", requires_grad=True)
+    out, S, S_out = torch.ones((2, 2, 64), device="cuda"), x["S"].cuda(), x["S"].cuda()
+    y = (w * out).sum()
+    call(kda, x, S=S, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.backward()
+    a, b = S._version, S_out._version
+    call(kda, x, S=S, S_out=S_out)
+    assert S._version == a and S_out._version > b            # (only read, written)
+    call(kda, x, S=S)
+    assert S._version > a
+    with torch.inference_mode():
+        S = x["S"].cuda()
+    call(kda, x, S=S)                                        # (has no version)
+
+
+@pytest.mark.parametrize("kda", [False, True])
 def test_tangents_are_refused(kda):
     import torch.autograd.forward_ad as fwd
     x = draw(np.random.default_rng(33), 2, 2, 64, "f32", kda, 2)
