@@ -76,8 +76,10 @@ int harts_cache_read(const harts_cache* cache, const int32_t* rows, int64_t n, v
  *
  * harts_gen_layout / harts_gen_tables (host) -- sizes, then tables.
  *   parent   [n_seg] parent segment or -1, any order; n_new [n_seg] >= 0.
- *   cap      [n_seg] rows that the segment may reach while the tables are in
- *            use: only a hint for how finely long segments are split.
+ *   cap      [n_seg] about how many rows the segment holds while the tables
+ *            are in use.  Results do not depend on it; how finely segments are
+ *            split does, by their shares of the whole: room that stays empty
+ *            takes splits from the segments that all rows wait for.
  *   Hq, Hkv  query and key heads; Hq a multiple of Hkv, query head h reads
  *            key head h / (Hq / Hkv).
  *   rows     [n_rows][2] out: the row table of the query rows (for

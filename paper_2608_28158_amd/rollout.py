@@ -118,6 +118,13 @@ class RolloutCache:
         self._free.extend(reversed(held))
         held.clear()
 
+    def held_rows(self):
+        """Rows [n_seg] that the reserved pages hold; of a cache without any, whose table the caller
+        fills itself, the table's columns for every segment."""
+        if not any(self._held):
+            return np.full(self.n_seg, self.pitch * PAGE, np.int64)
+        return np.array([len(held) * PAGE for held in self._held], np.int64)
+
     # -- rows ----------------------------------------------------------------
     def desc(self, layer: int):
         if not 0 <= layer < self.layers:
@@ -143,16 +150,21 @@ class RolloutBatch:
 
     parent [n_seg]: parent segment or -1; n_new [n_seg]: query rows at the end
     of every segment (0 for those that only serve others, or are unused).
-    capacity [n_seg]: rows that the segments may reach while the batch is in
-    use, a hint for splitting long ones (default: the pitch).  Query rows are
-    ordered by segment id, each segment's in order: ``rows`` is their table."""
+    capacity [n_seg]: about how many rows the segments hold while the batch is
+    in use.  Results do not depend on it, times do: the chip is shared out by
+    capacities, so that room which stays empty is taken from the segments that
+    all wait for.  (One token of 64 samples of a 65,000-row 8-bit prefix, tails
+    up to 3,900: 140 us by the present lengths, 556 with room for 32,768 more
+    rows a tail, 728 with room for 65,000.)  Default: what the pages reserved by
+    now hold; where much more is reserved than filled, pass the present lengths
+    and make the batch anew now and then.  Query rows are ordered by segment
+    id, each segment's in order: ``rows`` is their table."""
 
     def __init__(self, cache: RolloutCache, parent, n_new, q_heads: int, capacity=None):
         self.cache, self.q_heads, self.L = cache, int(q_heads), cache.L
         parent = np.ascontiguousarray(parent, dtype=np.int32)
         new = np.ascontiguousarray(n_new, dtype=np.int32)
-        cap = np.full(cache.n_seg, cache.pitch * PAGE, np.int64) if capacity is None else \
-            np.ascontiguousarray(capacity, dtype=np.int64)
+        cap = cache.held_rows() if capacity is None else np.ascontiguousarray(capacity, dtype=np.int64)
         for name, a in (("parent", parent), ("n_new", new), ("capacity", cap)):
             if a.shape != (cache.n_seg,):
                 raise ValueError(f"{name} must have one entry for each of the cache's {cache.n_seg} segments")

@@ -698,3 +698,19 @@ def test_inference_tensors_are_written():
             c.write(table([(0, i) for i in range(3)]), x, x)
             RolloutBatch(c, [-1], [3], 2).attend(x, out=out)
             assert torch.all(out == 1)
+
+
+def test_pages_held_are_the_default_capacity():
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    n = 9
+    c = new_cache(400, n, 300, 2, 64, "bf16")
+    held = [15000] + [100] * (n - 1)
+    for s, rows in enumerate(held):
+        c.reserve(s, rows)
+    parent, new = [-1] + [0] * (n - 1), [0] + [1] * (n - 1)
+    batch = RolloutBatch(c, parent, new, 4)
+    same = RolloutBatch(c, parent, new, 4, capacity=[-(-r // 64) * 64 for r in held])
+    assert torch.equal(batch._tab, same._tab)
+    # a table that the caller fills without reserve(): the most that it can hold
+    d = new_cache(4, n, 300, 2, 64, "bf16")
+    assert torch.equal(RolloutBatch(d, parent, new, 4)._tab, RolloutBatch(d, parent, new, 4, capacity=[300 * 64] * n)._tab)
