@@ -18,7 +18,8 @@ cache's; a fork of a sequence is two new segments below it, with no row copied.
     o, lse = batch.attend(q, layer)                # and their queries see it
 
 A batch's tables serve every step until the forest or n_new changes, so a step
-can be captured into a graph and replayed while the lengths grow.  Nothing here
+can be captured into a graph and replayed while the lengths grow, for as long
+as the program keeps the batch and the cache.  Nothing here
 is differentiable: inputs that require a gradient are refused while gradients
 are recorded, and inputs that carry a tangent (the training forms are tree_la,
 KdaRunner and harts_attn_*).  What a call writes counts as modified.
@@ -46,6 +47,24 @@ def _device(device):
 # of 1.2, of a small call's 5), where torch offers that.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+class _Streams:
+    """Tensors of an object that calls on any stream may use: their memory is
+    not handed out again before what those streams had queued when the object
+    was dropped has run."""
+
+    def __init__(self, device, tensors):
+        self.index, self.tensors = device.index, tensors
+        self.known = {_raw_stream(self.index)}       # (theirs, by the allocator)
+
+    def current(self):
+        stream = _raw_stream(self.index)
+        if stream not in self.known:
+            for t in self.tensors:
+                t.record_stream(torch.cuda.current_stream(self.index))
+            self.known.add(stream)
+        return stream
 
 
 class RolloutCache:
@@ -84,6 +103,7 @@ class RolloutCache:
                         for i in range(layers)]
         self._desc = [C.addressof(c) for c in self._layers]
         self._cells = tuple(t for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None)
+        self._streams = _Streams(self.device, self._cells + (self.pages, self.len))
 
     # -- pages (host bookkeeping) --------------------------------------------
     @property
@@ -106,6 +126,7 @@ class RolloutCache:
             return
         if more > len(self._free):
             raise RuntimeError(f"the cache is full: {more} pages wanted, {len(self._free)} free")
+        self._streams.current()
         new = [self._free.pop() for _ in range(more)]
         self.pages[seg, len(held):need] = torch.tensor(new, dtype=torch.int32, device=self.device)
         held.extend(new)
@@ -113,6 +134,7 @@ class RolloutCache:
     def release(self, seg: int):
         """Give the segment's pages back; it is empty afterwards."""
         held = self._held[self._seg(seg)]
+        self._streams.current()
         self.pages[seg].fill_(-1)
         self.len[seg].zero_()
         self._free.extend(reversed(held))
@@ -135,14 +157,12 @@ class RolloutCache:
         """Rows k, v [n, heads, d] (bf16) into the cache at ``rows`` [n, 2]
         (int32 segment and position, negative from the segment's end).  A row
         may be named once; entries that name no existing row are skipped."""
-        index = self.device.index
-        self._ext.cache_write(self.desc(layer), index, _raw_stream(index), self._cells, rows, k, v)
+        self._ext.cache_write(self.desc(layer), self.device.index, self._streams.current(), self._cells, rows, k, v)
 
     def read(self, rows, layer: int = 0):
         """(k, v) [n, heads, d] bf16: what the rows stand for, zeros where an
         entry names no existing row."""
-        index = self.device.index
-        return self._ext.cache_read(self.desc(layer), index, _raw_stream(index), rows)
+        return self._ext.cache_read(self.desc(layer), self.device.index, self._streams.current(), rows)
 
 
 class RolloutBatch:
@@ -182,6 +202,7 @@ class RolloutBatch:
         _lib.check(self.L.harts_gen_tables(*host, rows.ctypes.data, order.ctypes.data, items.ctypes.data,
                                            off.ctypes.data), "harts_gen_tables")
         self._tab = torch.from_numpy(host_tab).to(cache.device)
+        self._streams = _Streams(cache.device, (self._tab,))
         self.rows, order, items, off, self.n_new = part(self._tab)
         size = C.c_size_t()
         _lib.check(self.L.harts_gen_workspace_size(C.byref(self.sizes), self.q_heads, cache.d, C.byref(size)),
@@ -192,17 +213,21 @@ class RolloutBatch:
 
     def advance(self):
         """The segments' lengths grow by their new rows."""
+        self._streams.current()
+        self.cache._streams.current()
         self.cache.len.add_(self.n_new)
 
     def write(self, k, v, layer: int = 0):
         """The new rows' keys and values [n_rows, heads, d] into the cache."""
+        self._streams.current()
         self.cache.write(self.rows, k, v, layer)
 
     def attend(self, q, layer: int = 0, scale=None, out=None):
         """(o [n_rows, q_heads, d] bf16, lse [n_rows, q_heads] float32) of the
         new rows' queries; scale defaults to d ** -0.5."""
         c = self.cache
-        return c._ext.attend(c.desc(layer), *self._call, _raw_stream(c.device.index), q, scale, out)
+        self._streams.current()
+        return c._ext.attend(c.desc(layer), *self._call, c._streams.current(), q, scale, out)
 
 
 def la_step(q, k, v, g, S, S_out=None, idx_in=None, idx_out=None, row_off=None, scale=None, out=None):

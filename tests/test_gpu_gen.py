@@ -714,3 +714,34 @@ def test_pages_held_are_the_default_capacity():
     # a table that the caller fills without reserve(): the most that it can hold
     d = new_cache(4, n, 300, 2, 64, "bf16")
     assert torch.equal(RolloutBatch(d, parent, new, 4)._tab, RolloutBatch(d, parent, new, 4, capacity=[300 * 64] * n)._tab)
+
+
+def test_tables_outlive_their_batch_on_other_streams():
+    """A batch may be dropped while a call on a stream of the caller's is still to run: its tables' memory
+    is not handed out before that.  (The new tensors are not written.)"""
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    rng = np.random.default_rng(18)
+    parent, lens, new = FORESTS["long_prefix"]
+    c, K, V = filled(parent, lens, 2, 64, "bf16", rng)
+    q = bf16_values(rng.standard_normal((9, 4, 64)))
+    dev = q.cuda()
+    for use in ("attend", "write", "advance"):
+        batch = RolloutBatch(c, parent, new, 4, capacity=lens)
+        at, n = batch._tab.data_ptr(), batch._tab.numel()
+        k = torch.zeros((9, 2, 64), dtype=torch.bfloat16, device="cuda")
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(10_000_000)
+            if use == "attend":
+                o, lse = batch.attend(dev)
+            elif use == "write":
+                batch.write(k, k)
+            else:
+                batch.advance()
+        del batch
+        later = [torch.empty(n, dtype=torch.int32, device="cuda") for _ in range(3)]
+        assert at not in [t.data_ptr() for t in later], use
+        torch.cuda.synchronize()
+        if use == "attend":
+            compare(o, lse, forest_decode(parent, new, K, V, f64(q), 0.125), 64)
