@@ -71,7 +71,7 @@ int make(const char* where, int32_t n_seg, const int32_t* parent, const int32_t*
     P.row0[s + 1] = P.row0[s] + n_new[s];
   }
   const int64_t n_rows = P.row0[n_seg];
-  if (n_rows * Hq > INT32_MAX) {
+  if (n_rows > INT32_MAX / Hq) {
     set_error(std::string(where) + ": more than 2^31 - 1 (row, head) pairs");
     return HARTS_EUNSUPPORTED;
   }

@@ -150,6 +150,16 @@ def test_layout_refuses_null_and_size(L):
                               C.byref(sz)) == _lib.HARTS_EUNSUPPORTED
 
 
+def test_layout_refuses_rows_past_64_bits(L):
+    """(rows x heads, which wrapped around to a small or negative number)"""
+    from paper_2608_28158_amd import _lib
+    for n, heads in ((1 << 17, 65535), (1 << 18, 1 << 15)):
+        root, new, cap = np.full(n, -1, np.int32), np.full(n, 2 ** 31 - 1, np.int32), np.ones(n, np.int64)
+        sz = _lib.GenSizes()
+        assert L.harts_gen_layout(n, root.ctypes.data, new.ctypes.data, cap.ctypes.data, heads, 1,
+                                  C.byref(sz)) == _lib.HARTS_EUNSUPPORTED
+
+
 # ---------------------------------------------------------------------------
 # refusals of the device calls: nothing is enqueued, so any non-NULL aligned
 # addresses serve as pointers
