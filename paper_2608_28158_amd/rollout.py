@@ -49,6 +49,18 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+def _host_table(name, values, n, dtype):
+    """A table of one number for each of n segments, in a type that holds them as they are."""
+    given = np.asarray(values)
+    if given.shape != (n,):
+        raise ValueError(f"{name} must have one entry for each of the cache's {n} segments")
+    with np.errstate(invalid="ignore"):
+        a = np.ascontiguousarray(given, dtype=dtype)
+    if not np.array_equal(a, given):
+        raise ValueError(f"{name} must hold whole numbers of {np.dtype(dtype).name}")
+    return a
+
+
 class _Streams:
     """Tensors of an object that calls on any stream may use: their memory is
     not handed out again before what those streams had queued when the object
@@ -182,12 +194,11 @@ class RolloutBatch:
 
     def __init__(self, cache: RolloutCache, parent, n_new, q_heads: int, capacity=None):
         self.cache, self.q_heads, self.L = cache, int(q_heads), cache.L
-        parent = np.ascontiguousarray(parent, dtype=np.int32)
-        new = np.ascontiguousarray(n_new, dtype=np.int32)
-        cap = cache.held_rows() if capacity is None else np.ascontiguousarray(capacity, dtype=np.int64)
-        for name, a in (("parent", parent), ("n_new", new), ("capacity", cap)):
-            if a.shape != (cache.n_seg,):
-                raise ValueError(f"{name} must have one entry for each of the cache's {cache.n_seg} segments")
+        if self.q_heads != q_heads or self.q_heads > 65535:
+            raise ValueError(f"q_heads must be a whole number of at most 65535, got {q_heads}")
+        parent = _host_table("parent", parent, cache.n_seg, np.int32)
+        new = _host_table("n_new", n_new, cache.n_seg, np.int32)
+        cap = cache.held_rows() if capacity is None else _host_table("capacity", capacity, cache.n_seg, np.int64)
         host = (cache.n_seg, parent.ctypes.data, new.ctypes.data, cap.ctypes.data, self.q_heads, cache.heads)
         self.sizes = _lib.GenSizes()
         _lib.check(self.L.harts_gen_layout(*host, C.byref(self.sizes)), "harts_gen_layout")

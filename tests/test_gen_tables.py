@@ -321,6 +321,25 @@ def test_python_calls_refuse_tensors_of_the_cpu(L):
         RolloutCache(2, 2, 1, 2, 64, device="cpu")
 
 
+def test_host_tables_are_not_cut_to_size():
+    """Numbers that the tables' types do not hold are refused, not wrapped around or cut off."""
+    import torch
+    from paper_2608_28158_amd.rollout import _host_table
+    for good in ([-1, 0, 7], np.array([-1, 0, 7], np.int64), np.array([-1.0, 0.0, 7.0]), torch.tensor([-1, 0, 7])):
+        a = _host_table("parent", good, 3, np.int32)
+        assert a.dtype == np.int32 and a.flags.c_contiguous and list(a) == [-1, 0, 7]
+    assert list(_host_table("n_new", np.arange(6)[::2], 3, np.int32)) == [0, 2, 4]
+    assert _host_table("capacity", [2 ** 63 - 1], 1, np.int64)[0] == 2 ** 63 - 1
+    for bad in (np.array([2 ** 32 + 1]), np.array([-2 ** 32]), [1.5], [float("nan")], np.array([2 ** 31]), [1e300]):
+        with pytest.raises(ValueError, match="whole numbers of int32"):
+            _host_table("n_new", bad, 1, np.int32)
+    with pytest.raises(ValueError, match="whole numbers of int64"):
+        _host_table("capacity", np.array([2 ** 64 - 1], np.uint64), 1, np.int64)
+    for shape in ([1], [1, 2, 3], [[1, 2]], 1):
+        with pytest.raises(ValueError, match="one entry for each"):
+            _host_table("n_new", shape, 2, np.int32)
+
+
 # ---------------------------------------------------------------------------
 # the oracle's rounding, against every code
 # ---------------------------------------------------------------------------
