@@ -90,6 +90,28 @@ def test_tables_cover_every_row_and_key_once(L, seed):
         assert list(dict.fromkeys(segs)) == chain(parent, rows[r][0])
 
 
+@pytest.mark.parametrize("seed", range(8))
+def test_items_carry_new_rows_and_divisors(L, seed):
+    """Every item's own new rows, and the multiplier and shift that divide by its splits, at the edges
+    of quotients up to the largest number."""
+    rng = np.random.default_rng(100 + seed)
+    n = int(rng.integers(1, 20))
+    parent = random_forest(rng, n)
+    n_new = rng.integers(0, 1 + int(rng.choice([1, 3, 200])), n)
+    n_new[-1] = max(1, n_new[-1])
+    cap = rng.choice([0, 1, 63, 900, 5000, 70000, 10 ** 9], n)
+    _, _, _, items, _ = tables(L, parent, n_new, cap, 8, 2)
+    assert len(items)
+    for seg, _, _, _, _, splits, new, _, _, _, mul, shift in (map(int, x) for x in items):
+        assert new == n_new[seg]
+        mul &= 2 ** 32 - 1
+        near = {0, 1, splits - 1, splits, splits + 1, 2 ** 31 - 1, (2 ** 31 - 1) // splits * splits}
+        near |= {k * splits + e for k in (2, 3, 1000, 65536) for e in (-1, 0, 1)}
+        for x in near:
+            if 0 <= x < 2 ** 31:
+                assert x * mul >> shift == x // splits, (x, splits)
+
+
 def test_a_deep_chain_and_many_segments(L):
     n = 4000
     parent = np.arange(-1, n - 1)

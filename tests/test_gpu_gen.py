@@ -745,3 +745,66 @@ def test_tables_outlive_their_batch_on_other_streams():
         torch.cuda.synchronize()
         if use == "attend":
             compare(o, lse, forest_decode(parent, new, K, V, f64(q), 0.125), 64)
+
+
+def test_log_sums_by_graph_replay():
+    """The log-sums of captured steps, while the lengths grow."""
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    rng = np.random.default_rng(16)
+    parent, lens, new = [-1, 0, 0], [600, 60, 1], [0, 1, 2]
+    c, K, V = filled(parent, lens, 2, 64, "bf16", rng)
+    batch = RolloutBatch(c, parent, new, 4, capacity=[600, 80, 80])
+    k, v = (torch.zeros((3, 2, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.zeros((3, 4, 64), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        batch.advance()
+        batch.write(k, v)
+        o, lse = batch.attend(q)
+    for t in range(4):
+        fresh = [bf16_values(rng.standard_normal(tuple(x.shape))) for x in (q, k, v)]
+        for x, y in zip((q, k, v), fresh):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        for j, (s, _) in enumerate(batch.rows.tolist()):
+            K[s] = np.concatenate([K[s], f64(fresh[1])[j:j + 1]])
+            V[s] = np.concatenate([V[s], f64(fresh[2])[j:j + 1]])
+        compare(o, lse, forest_decode(parent, new, K, V, f64(fresh[0]), 0.125), 64)
+        eager = batch.attend(q)
+        assert torch.equal(eager[0], o) and torch.equal(eager[1], lse)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_training_attention_gives_the_same_rows(d):
+    """The rows of a finished tree, attended through the cache a segment at a time, against harts_attn_fwd
+    over the tree.  Both round the same things (weights to bf16, sums in float32, the output), so they differ
+    by at most twice the bound of one."""
+    from paper_2608_28158_amd import _lib
+    from paper_2608_28158_amd.plan import HartsPlan
+    from paper_2608_28158_amd.rollout import RolloutBatch
+    from tests.test_gpu_attn import run_attn
+    rng = np.random.default_rng(17)
+    parent, lens, H = [-1, 0, 0, 1], [150, 70, 20, 65], 2
+    n, C = len(lens), sum(lens)
+    plan = HartsPlan(parent, lens, 64)
+    phys = [np.arange(lens[s]) + int(plan["seg_row"][s]) for s in range(n)]
+    q, k, v = (bf16_values(rng.standard_normal((C, H, d))) for _ in range(3))
+    trained = run_attn(_lib.lib(), plan, q.cuda(), k.cuda(), v.cuda(), torch.zeros_like(q).cuda(), H, d, d ** -0.5)
+    c = new_cache(10, n, 3, H, d, "bf16")
+    K, V = [], []
+    for s in range(n):                                       # parents come first
+        c.reserve(s, lens[s])
+        c.len[s] = lens[s]
+        new = [lens[s] if i == s else 0 for i in range(n)]
+        batch = RolloutBatch(c, parent, new, H, capacity=lens)
+        batch.write(k[phys[s]].cuda(), v[phys[s]].cuda())
+        K.append(f64(k[phys[s]]))
+        V.append(f64(v[phys[s]]))
+        o, lse = batch.attend(q[phys[s]].cuda())
+        ref = forest_decode(parent[:s + 1], new[:s + 1], K, V, f64(q[phys[s]]), d ** -0.5)
+        compare(o, lse, ref, d)
+        tol_o, tol_l = bounds(ref[0], ref[2], ref[3], ref[1], d)
+        assert np.all(np.abs(f64(o) - f64(trained["o"])[phys[s]]) <= 2 * tol_o)
+        assert np.all(np.abs(f64(lse) - f64(trained["lse"])[phys[s]]) <= 2 * tol_l)
