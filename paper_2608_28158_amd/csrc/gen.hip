@@ -117,16 +117,21 @@ __device__ inline u32x2 quantise(const u32x4& x, u32& exponent) {
   }
   const int b = static_cast<int>(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
   exponent = b < 1 ? 1u : static_cast<u32>(b);
-  const float inv = exp_scale(254u - exponent), most = exponent == 247u ? 240.f : 448.f;
+  const float inv = exp_scale(254u - exponent);
   float f[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32 bits = ((x[i] >> (16 * h)) & 0xffffu) << 16;
-      const float y = __builtin_amdgcn_fmed3f(__builtin_bit_cast(float, bits) * inv, -most, most);
+      const float y = __builtin_bit_cast(float, bits) * inv;
       f[2 * i + h] = (bits & 0x7f800000u) == 0x7f800000u ? __builtin_nanf("") : y;
     }
+  if (__builtin_expect(__any(exponent == 247u), 0)) {
+    const float most = exponent == 247u ? 240.f : 448.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = f[e] > most ? most : f[e] < -most ? -most : f[e];
+  }
   u32x2 out;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -433,6 +438,15 @@ struct RowState {
     for (int j = 0; j < DT; ++j) acc[j] *= f;
   }
   __device__ inline float zero_point() const { return ref == -INFINITY ? 0.f : ref; }
+  // what the accumulators are to be multiplied by; those of a row without weight
+  // are set to zeros (they are 0 times an infinity where its keys hold one), out
+  // of the way: in line, the selects took a short call 0.17 of 8.3 us
+  __device__ inline float inverse() {
+    if (__builtin_expect(__any(sum == 0.f), 0)) {
+      if (sum == 0.f) clear();
+    }
+    return sum == 0.f ? 0.f : 1.f / sum;
+  }
 };
 
 // Values that are not finite, in steps whose keys some rows of a wave see and
@@ -617,8 +631,7 @@ __device__ inline void gen_few(const GenArgs& A, Scalars it, int hk, int wave, i
 
   if (parts == 1) {
     const int64_t rh = static_cast<int64_t>(row) * A.Hq + head;
-    if (st.sum == 0.f) st.clear();                  // (no weight at all: not 0 times an infinite value)
-    const float f = st.sum == 0.f ? 0.f : 1.f / st.sum;
+    const float f = st.inverse();
     u32 out[D / 8];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -941,8 +954,7 @@ __device__ inline void gen_many(const GenArgs& A, Scalars it, int hk, int wave, 
     const int32_t p0 = A.part_off[row], parts = A.part_off[row + 1] - p0;
     if (parts == 1) {
       const int64_t rh = static_cast<int64_t>(row) * A.Hq + head;
-      if (st[a].sum == 0.f) st[a].clear();     // (as in gen_few)
-      const float f = st[a].sum == 0.f ? 0.f : 1.f / st[a].sum;
+      const float f = st[a].inverse();
 #pragma unroll
       for (int j = 0; j < DT; ++j) Vec4<bf16>::store(A.o + rh * D + 16 * j + 4 * g, st[a].acc[j] * f);
       if (A.lse && g == 0) A.lse[rh] = log_sum(st[a].ref, st[a].sum);
@@ -1046,7 +1058,7 @@ __global__ __launch_bounds__(GEN_THR) void k_gen_join(GenArgs A, int64_t n) {
     }
   }
   if (parts <= 1) return;
-  if (sum == 0.f) acc = f32x4{0.f, 0.f, 0.f, 0.f};   // (as in gen_few)
+  if (sum == 0.f) acc = f32x4{0.f, 0.f, 0.f, 0.f};   // (as in RowState)
   Vec4<bf16>::store(A.o + rh * D + c, acc * (sum == 0.f ? 0.f : 1.f / sum));
   if (A.lse && c == 0) A.lse[rh] = log_sum(ref, sum);
 }

@@ -9,6 +9,7 @@
 #include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <pybind11/pybind11.h>
+#include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <cmath>
@@ -88,7 +89,7 @@ const int32_t* ints(const OptTensor& t) { return static_cast<const int32_t*>(ptr
 
 const harts_cache* cache_at(uintptr_t p) { return reinterpret_cast<const harts_cache*>(p); }
 
-// cells: the tensors that hold the cache
+// cells: the tensors that hold the cache (the package's own tuple)
 void cache_write(uintptr_t desc, int64_t device, uintptr_t stream, const py::tuple& cells, const Tensor& rows,
                  const Tensor& k, const Tensor& v) {
   const harts_cache* c = cache_at(desc);
@@ -100,7 +101,7 @@ void cache_write(uintptr_t desc, int64_t device, uintptr_t stream, const py::tup
   const c10::DeviceGuard on(check.device);
   ok(L.cache_write(c, rows.const_data_ptr<int32_t>(), n, k.const_data_ptr(), v.const_data_ptr(),
                    reinterpret_cast<void*>(stream)), "harts_cache_write");
-  for (const py::handle t : cells) written(t.cast<Tensor>());
+  for (const py::handle t : cells) written(THPVariable_Unpack(t.ptr()));
 }
 
 py::tuple cache_read(uintptr_t desc, int64_t device, uintptr_t stream, const Tensor& rows) {

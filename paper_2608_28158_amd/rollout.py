@@ -61,25 +61,29 @@ def _host_table(name, values, n, dtype):
     return a
 
 
-class _Streams:
-    """Tensors of an object that calls on any stream may use: their memory is
+class _OnStreams:
+    """An object with tensors that calls on any stream may use: their memory is
     not handed out again before what those streams had queued when the object
-    was dropped has run."""
+    was dropped has run.  ``_known`` are the streams it has been used on."""
 
-    def __init__(self, device, tensors):
-        self.index, self.tensors = device.index, tensors
-        self.known = {_raw_stream(self.index)}       # (theirs, by the allocator)
+    def _keep(self, index, tensors):
+        self._index, self._kept = index, tensors
+        self._known = {_raw_stream(index)}           # (theirs, by the allocator)
 
-    def current(self):
-        stream = _raw_stream(self.index)
-        if stream not in self.known:
-            for t in self.tensors:
-                t.record_stream(torch.cuda.current_stream(self.index))
-            self.known.add(stream)
+    def _meet(self, stream):
+        for t in self._kept:
+            t.record_stream(torch.cuda.current_stream(self._index))
+        self._known.add(stream)
+
+    def _stream(self):
+        """The current stream, known from now on."""
+        stream = _raw_stream(self._index)
+        if stream not in self._known:
+            self._meet(stream)
         return stream
 
 
-class RolloutCache:
+class RolloutCache(_OnStreams):
     """Paged keys and values of ``layers`` layers (harts_cache): ``n_pages``
     pages of 64 rows shared by ``n_seg`` segments of up to ``pitch`` pages.
     kind "bf16" or "e4m3".  The tensors are the cache: k, v
@@ -115,7 +119,7 @@ class RolloutCache:
                         for i in range(layers)]
         self._desc = [C.addressof(c) for c in self._layers]
         self._cells = tuple(t for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None)
-        self._streams = _Streams(self.device, self._cells + (self.pages, self.len))
+        self._keep(self.device.index, self._cells + (self.pages, self.len))
 
     # -- pages (host bookkeeping) --------------------------------------------
     @property
@@ -138,7 +142,7 @@ class RolloutCache:
             return
         if more > len(self._free):
             raise RuntimeError(f"the cache is full: {more} pages wanted, {len(self._free)} free")
-        self._streams.current()
+        self._stream()
         new = [self._free.pop() for _ in range(more)]
         self.pages[seg, len(held):need] = torch.tensor(new, dtype=torch.int32, device=self.device)
         held.extend(new)
@@ -146,7 +150,7 @@ class RolloutCache:
     def release(self, seg: int):
         """Give the segment's pages back; it is empty afterwards."""
         held = self._held[self._seg(seg)]
-        self._streams.current()
+        self._stream()
         self.pages[seg].fill_(-1)
         self.len[seg].zero_()
         self._free.extend(reversed(held))
@@ -169,15 +173,15 @@ class RolloutCache:
         """Rows k, v [n, heads, d] (bf16) into the cache at ``rows`` [n, 2]
         (int32 segment and position, negative from the segment's end).  A row
         may be named once; entries that name no existing row are skipped."""
-        self._ext.cache_write(self.desc(layer), self.device.index, self._streams.current(), self._cells, rows, k, v)
+        self._ext.cache_write(self.desc(layer), self._index, self._stream(), self._cells, rows, k, v)
 
     def read(self, rows, layer: int = 0):
         """(k, v) [n, heads, d] bf16: what the rows stand for, zeros where an
         entry names no existing row."""
-        return self._ext.cache_read(self.desc(layer), self.device.index, self._streams.current(), rows)
+        return self._ext.cache_read(self.desc(layer), self._index, self._stream(), rows)
 
 
-class RolloutBatch:
+class RolloutBatch(_OnStreams):
     """The new rows of one step over a cache's forest (harts_gen_tables).
 
     parent [n_seg]: parent segment or -1; n_new [n_seg]: query rows at the end
@@ -213,7 +217,8 @@ class RolloutBatch:
         _lib.check(self.L.harts_gen_tables(*host, rows.ctypes.data, order.ctypes.data, items.ctypes.data,
                                            off.ctypes.data), "harts_gen_tables")
         self._tab = torch.from_numpy(host_tab).to(cache.device)
-        self._streams = _Streams(cache.device, (self._tab,))
+        cache._stream()
+        self._keep(cache._index, (self._tab,))
         self.rows, order, items, off, self.n_new = part(self._tab)
         size = C.c_size_t()
         _lib.check(self.L.harts_gen_workspace_size(C.byref(self.sizes), self.q_heads, cache.d, C.byref(size)),
@@ -222,23 +227,25 @@ class RolloutBatch:
         self._call = (C.addressof(self.sizes), items.data_ptr(), order.data_ptr(), off.data_ptr(), self.q_heads,
                       self.ws_bytes, cache.device.index)
 
+    def _meet(self, stream):
+        super()._meet(stream)
+        self.cache._stream()                         # (so the cache knows all streams that the batch does)
+
     def advance(self):
         """The segments' lengths grow by their new rows."""
-        self._streams.current()
-        self.cache._streams.current()
+        self._stream()
         self.cache.len.add_(self.n_new)
 
     def write(self, k, v, layer: int = 0):
         """The new rows' keys and values [n_rows, heads, d] into the cache."""
-        self._streams.current()
-        self.cache.write(self.rows, k, v, layer)
+        c = self.cache
+        c._ext.cache_write(c.desc(layer), c._index, self._stream(), c._cells, self.rows, k, v)
 
     def attend(self, q, layer: int = 0, scale=None, out=None):
         """(o [n_rows, q_heads, d] bf16, lse [n_rows, q_heads] float32) of the
         new rows' queries; scale defaults to d ** -0.5."""
         c = self.cache
-        self._streams.current()
-        return c._ext.attend(c.desc(layer), *self._call, c._streams.current(), q, scale, out)
+        return c._ext.attend(c.desc(layer), *self._call, self._stream(), q, scale, out)
 
 
 def la_step(q, k, v, g, S, S_out=None, idx_in=None, idx_out=None, row_off=None, scale=None, out=None):
