@@ -240,7 +240,8 @@ extern "C" int harts_gen_tables(int32_t n_seg, const int32_t* parent, const int3
 }
 
 extern "C" int harts_gen_workspace_size(const harts_gen_sizes* sizes, int32_t Hq, int32_t d, size_t* bytes) {
-  if (!sizes || !bytes || Hq < 1 || sizes->n_parts < 0 || (d != 64 && d != 128)) {
+  if (!sizes || !bytes || Hq < 1 || Hq > 65535 || sizes->n_parts < 0 || sizes->n_parts > INT32_MAX ||
+      (d != 64 && d != 128)) {
     set_error("harts_gen_workspace_size: NULL argument or bad sizes");
     return HARTS_EINVAL;
   }

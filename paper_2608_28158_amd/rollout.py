@@ -96,6 +96,8 @@ class RolloutCache(_OnStreams):
             raise ValueError("kind must be 'bf16' or 'e4m3'")
         if min(n_pages, n_seg, pitch, heads, layers) < 1 or d not in (64, 128):
             raise ValueError("need at least one page, segment, column, head and layer, and d in {64, 128}")
+        if max(n_pages, n_seg, pitch) > 2 ** 31 - 1 or heads > 65535:
+            raise ValueError("need at most 2^31 - 1 pages, segments and columns, and 65535 heads")
         self.L, self._ext, self.device = _lib.rollout(), _lib.rollout_binding(), _device(device)
         self.n_pages, self.n_seg, self.pitch, self.heads, self.d = n_pages, n_seg, pitch, heads, d
         self.kind, self.layers = kind, layers

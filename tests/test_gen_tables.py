@@ -343,6 +343,19 @@ def test_python_calls_refuse_tensors_of_the_cpu(L):
         RolloutCache(2, 2, 1, 2, 64, device="cpu")
 
 
+def test_sizes_past_32_bits_are_refused(L):
+    from paper_2608_28158_amd import _lib
+    from paper_2608_28158_amd.rollout import RolloutCache
+    b = C.c_size_t()
+    for parts, heads in ((2 ** 31, 4), (2 ** 62, 4), (8, 65536), (8, 2 ** 30)):
+        assert L.harts_gen_workspace_size(C.byref(_lib.GenSizes(4, 4, parts, 4)), heads, 64, C.byref(b)) == _lib.HARTS_EINVAL
+    assert L.harts_gen_workspace_size(C.byref(_lib.GenSizes(4, 4, 2 ** 31 - 1, 4)), 65535, 128, C.byref(b)) == _lib.HARTS_OK
+    assert b.value == (2 ** 31 - 1) * 65535 * 130 * 4
+    for over in (dict(n_pages=2 ** 32 + 1), dict(n_seg=2 ** 31), dict(pitch=2 ** 32 + 1), dict(heads=65536)):
+        with pytest.raises(ValueError, match="at most"):
+            RolloutCache(**{**dict(n_pages=1, n_seg=1, pitch=1, heads=1, d=64), **over})
+
+
 def test_host_tables_are_not_cut_to_size():
     """Numbers that the tables' types do not hold are refused, not wrapped around or cut off."""
     import torch
