@@ -77,8 +77,8 @@ int harts_cache_read(const harts_cache* cache, const int32_t* rows, int64_t n, v
  * harts_gen_layout / harts_gen_tables (host) -- sizes, then tables.
  *   parent   [n_seg] parent segment or -1, any order; n_new [n_seg] >= 0.
  *   cap      [n_seg] about how many rows the segment holds while the tables
- *            are in use.  Results do not depend on it; how finely segments are
- *            split does, by their shares of the whole: room that stays empty
+ *            are in use: how finely they are split, by their shares of the
+ *            whole.  Results differ by rounding only, but room that stays empty
  *            takes splits from the segments that all rows wait for.
  *   Hq, Hkv  query and key heads; Hq a multiple of Hkv, query head h reads
  *            key head h / (Hq / Hkv).
@@ -100,7 +100,9 @@ int harts_cache_read(const harts_cache* cache, const int32_t* rows, int64_t n, v
  *   float32 or NULL; sizes, items, order, part_off from the tables; ws of
  *   harts_gen_workspace_size bytes.  A row that sees no key, or only keys of
  *   score -infinity, gets zeros and lse = -infinity; a key that a row does
- *   not see has no influence on it, whatever its values.  Deterministic.
+ *   not see has no influence on it, whatever its values.  Weights are summed
+ *   up to 2^8 times too large before they are normalised: values that 2^8 and
+ *   the number of keys bring past float32 may give infinities.  Deterministic.
  * All: HARTS_EINVAL (NULL, misaligned, small workspace), HARTS_EUNSUPPORTED
  * (d, heads, kind), HARTS_EHIP.  Device calls are asynchronous and can be
  * captured; o, lse and ws overlap no other argument.
@@ -138,7 +140,8 @@ int harts_gen_attn(const harts_cache* cache, const harts_gen_sizes* sizes, const
  *   S_out       float32 [n_out][H][d][d]; idx_out likewise; outside
  *               [0, n_out) the last state is not kept.  Where an index of
  *               idx_out repeats an earlier one, that sequence writes no
- *               state and its outputs are NaN.
+ *               state and its outputs are NaN (found by reading the earlier
+ *               ones: free up to thousands of sequences, quadratic beyond).
  *   S_out may be S_in itself if idx_out is idx_in and n_out = n_in, for an
  *   update in place; otherwise the two must not overlap.
  * Rows behind the last sequence, entries that no index names and outputs of

@@ -39,7 +39,9 @@
 // the largest weight that leaves sums and products far from overflow; most
 // steps then have no rescale and no exchange between lanes.  Weights are
 // rounded to bf16 for the second product (half a step, 2^-8 of each, as any
-// bf16 operand); their sum is taken before that in float32.
+// bf16 operand); their sum is taken before that in float32.  o is off by 0.0023
+// of its norm so, by 0.0017 with float32 weights (its own rounding alone), which
+// would take a second product for what bf16 leaves of them.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

@@ -2,7 +2,7 @@
 // checks of the arguments, allocation of the results and the call, in one step.
 // A generated token is many small calls, and each of these took 5 to 7 us of
 // Python around a 3 us launch (one linear-attention step of one sequence: 11.3 us,
-// of which the kernel is 4.3).  The library's functions are handed over by
+// of which the kernel takes 3; so 5.1).  The library's functions are handed over by
 // address (bind), so that it is the one library that the package has loaded.
 #include <ATen/Functions.h>
 #include <ATen/core/Tensor.h>

@@ -189,14 +189,15 @@ class RolloutBatch(_OnStreams):
     parent [n_seg]: parent segment or -1; n_new [n_seg]: query rows at the end
     of every segment (0 for those that only serve others, or are unused).
     capacity [n_seg]: about how many rows the segments hold while the batch is
-    in use.  Results do not depend on it, times do: the chip is shared out by
-    capacities, so that room which stays empty is taken from the segments that
-    all wait for.  (One token of 64 samples of a 65,000-row 8-bit prefix, tails
-    up to 3,900: 140 us by the present lengths, 556 with room for 32,768 more
-    rows a tail, 728 with room for 65,000.)  Default: what the pages reserved by
-    now hold; where much more is reserved than filled, pass the present lengths
-    and make the batch anew now and then.  Query rows are ordered by segment
-    id, each segment's in order: ``rows`` is their table."""
+    in use.  Results differ by rounding only, times by much more: the chip is
+    shared out by capacities, so that room which stays empty is taken from the
+    segments that all wait for.  (One token of 64 samples of a 65,000-row
+    8-bit prefix, tails up to 3,900: 140 us by the present lengths, 556 with
+    room for 32,768 more rows a tail, 728 with room for 65,000.)  Default:
+    what the pages reserved by now hold; where much more is reserved than
+    filled, pass the present lengths and make the batch anew now and then.
+    Query rows are ordered by segment id, each segment's in order: ``rows`` is
+    their table."""
 
     def __init__(self, cache: RolloutCache, parent, n_new, q_heads: int, capacity=None):
         self.cache, self.q_heads, self.L = cache, int(q_heads), cache.L
@@ -255,7 +256,11 @@ def la_step(q, k, v, g, S, S_out=None, idx_in=None, idx_out=None, row_off=None, 
     [rows, H, d] and g [rows, H] for each sequence, or sequence i's rows
     [row_off[i], row_off[i + 1]) one after the other.  States start from
     S[idx_in[i]] and end in S_out[idx_out[i]] (no index: i; no S_out: in
-    place).  Several sequences may start from one state: a fork.  Returns o."""
+    place).  Several sequences may start from one state: a fork.  A slot named
+    again by idx_out gets no second state, and that sequence's outputs are NaN
+    (the test is quadratic in sequences: free up to thousands, a quarter of the
+    call at 16,384).  Returns o; rows that no sequence names keep what ``out``
+    held, and without ``out`` they are uninitialised."""
     return _lib.rollout_binding().step(False, q, k, v, g, None, S, S_out, idx_in, idx_out, row_off, scale, out,
                                        _raw_stream)
 
